@@ -416,7 +416,7 @@ typedef struct {
  * its row and smaller ones to within 2^-17 of that one; cached keys enter as they are, sums are fp32.  The weights and the values are f16 in the product,
  * the values relative to the largest one of their tile (64 tokens of the prefix, or 64 kept nodes): bits below 2^-33 of that are lost, and values below
  * 2^-84 count as zero.  Tree values of 2^20 and more, and those that are not finite, stay out of that: they reach the rows that see them, in fp32 (from 2^100
- * on as infinities), and no other; beside them such a row keeps its other values to 2^-33 of them.  A query, a tree key or a cached row with a value that is not finite makes NaN of the rows that see it.
+ * on as infinities), and no other; beside them such a row keeps its other values to 2^-38 of them.  A query, a tree key or a cached row with a value that is not finite makes NaN of the rows that see it.
  * n_pages * hkv * page_size <= 2^31 - 1, batch * hkv <= 65535. */
 hs_status hs_tree_verify_attention_paged(hs_ctx* ctx, const hs_pruned_tree* pruned, const hs_kv_cache* cache,
                                          const hs_paged_attn_desc* desc, const void* q, const void* k_tree,

@@ -50,7 +50,7 @@
 #define PG_GROUPS 4                                 // groups of converters, and f16 tiles of V
 #define PG_EXPS 8                                   // tiles whose scales are kept
 #define PG_LIFT 6.f                                 // P = 2^(6 + ..): f16 then keeps weights down to 2^-30 of the largest
-#define PG_ROW_STRIDE (HS_HEAD_DIM * 2 + 16)        // a pushed partial row: 128 f16 of O / l / 2^B, {max, sum, B}
+#define PG_ROW_STRIDE (HS_HEAD_DIM * 2 + 16)        // a pushed partial row: 128 f16 of O 2^-k, {max, sum, k}
 #define PG_THREADS 640
 #define PG_REGS 96                                  // of a thread at launch
 #define PG_SM_THREADS 256                           // softmax threads: row = tid & 127, stream = tid >> 7
@@ -77,8 +77,8 @@ struct Layout {
     static constexpr int recv = WIDE ? k : q;
     static constexpr int scale = q + (!WIDE && recv_bytes > q_bytes ? recv_bytes : q_bytes);      // scale bytes of the units: V's 64, K's 64
     static constexpr int bar = scale + units * 2 * PG_BN;
-    static constexpr int x = bar + 512;              // the streams' maxima and sums, [2][128] each, and largest B
-    static constexpr int exps = x + 4 * PG_BM * 4 + 16;   // per tile {B, 2^-B}
+    static constexpr int x = bar + 512;              // the streams' maxima and sums, [2][128] each
+    static constexpr int exps = x + 4 * PG_BM * 4;   // per tile {B, 2^-B}
     static constexpr int ks = exps + 2 * PG_EXPS * 4;     // per tile the keys' scales
     static constexpr int qs = ks + PG_EXPS * PG_BN * 4;   // the query rows' scales
     static constexpr int red = qs + rows * 4;             // maxima of the softmax warps
@@ -166,10 +166,6 @@ __device__ __forceinline__ unsigned int pair_amax(unsigned int w) { return max(w
 // to the rows that see it at the end.  A pair without such values:
 #define PG_APART 0x49800000u                        // 2^20, the bits
 #define PG_ENDLESS 0x71800000u                      // 2^100: weights of up to 2^14 times more would leave fp32, it counts as infinite
-__device__ __forceinline__ unsigned int apart_max(unsigned int w) {
-    const unsigned int lo = w << 16 & 0x7fff0000u, hi = w & 0x7fff0000u;
-    return max(lo < PG_ENDLESS ? lo : 0u, hi < PG_ENDLESS ? hi : 0u);
-}
 __device__ __forceinline__ unsigned int near_or_zero(unsigned int w) {
     return ((w << 16 & 0x7fff0000u) >= PG_APART ? 0u : w & 0xffffu) | ((w & 0x7fff0000u) >= PG_APART ? 0u : w & 0xffff0000u);
 }
@@ -234,7 +230,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     constexpr int COLS = PG_BN / REP;                      // columns of a tile that a thread takes
     extern __shared__ unsigned char smem_raw[];
     __shared__ int s_seq;
-    __shared__ unsigned int s_tmem, s_odd[4], s_apart;              // s_odd: tree keys whose value stays out of the product somewhere
+    __shared__ unsigned int s_tmem, s_odd[4];                       // s_odd: tree keys whose value stays out of the product somewhere
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned int base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* gen = smem_raw + (base - smem_u32(smem_raw));
@@ -249,7 +245,6 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
         tmem_relinquish();
     }
     if (tid < 4) s_odd[tid] = 0u;
-    if (tid == 4) s_apart = 0u;
     if (tid == 32) {
         for (int i = 0; i < PG_KEYS; ++i) {                  // keys there, S issued
             mbar_init(bar_k + 8 * i, 1);
@@ -456,7 +451,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 unsigned char* tile = gen + Y::v + t * PG_TILE_BYTES;
                 unsigned int a = 0u;
                 const int keys16 = min(PG_BN, (nk - (g0 + t) * PG_BN + 15) & ~15);       // (those behind them are masked, and zeros)
-                    [[maybe_unused]] uint4 v[PG_BN / 16];
+                [[maybe_unused]] uint4 v[PG_BN / 16];
                 if constexpr (REP > 1) {                     // a row at a time, read again below
 #pragma unroll 1
                     for (int row = ct8 >> 4; row < keys16; row += 16) {
@@ -465,7 +460,6 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                         uint4 x = *at;
                         unsigned int m = max(max(pair_amax(x.x), pair_amax(x.y)), max(pair_amax(x.z), pair_amax(x.w)));
                         if (m >= PG_APART) {
-                            atomicMax(&s_apart, max(max(apart_max(x.x), apart_max(x.y)), max(apart_max(x.z), apart_max(x.w))));
                             x = make_uint4(near_or_zero(x.x), near_or_zero(x.y), near_or_zero(x.z), near_or_zero(x.w));
                             m = max(max(pair_amax(x.x), pair_amax(x.y)), max(pair_amax(x.z), pair_amax(x.w)));
                             *at = x;
@@ -483,8 +477,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                         v[j] = row < keys16 ? *reinterpret_cast<const uint4*>(tile + pg_off(PG_BN, row, sub)) : make_uint4(0u, 0u, 0u, 0u);
                         unsigned int m = max(max(pair_amax(v[j].x), pair_amax(v[j].y)), max(pair_amax(v[j].z), pair_amax(v[j].w)));
                         if (m >= PG_APART) {
-                            atomicMax(&s_apart, max(max(apart_max(v[j].x), apart_max(v[j].y)), max(apart_max(v[j].z), apart_max(v[j].w))));
-                        v[j] = make_uint4(near_or_zero(v[j].x), near_or_zero(v[j].y), near_or_zero(v[j].z), near_or_zero(v[j].w));
+                            v[j] = make_uint4(near_or_zero(v[j].x), near_or_zero(v[j].y), near_or_zero(v[j].z), near_or_zero(v[j].w));
                             m = max(max(pair_amax(v[j].x), pair_amax(v[j].y)), max(pair_amax(v[j].z), pair_amax(v[j].w)));
                             const int key = (g0 + t) * PG_BN + row;
                             atomicOr(&s_odd[key >> 5], 1u << (key & 31));
@@ -780,7 +773,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
 
     // The stream's tiles.  As soon as S is in registers its buffer is handed back.  The stream's P buffer and O were last used by its last O += P V, which is
     // waited for before they are touched.  Both barriers are asked ahead of other work: an answer takes 123 clocks.
-    float mrun = -CUDART_INF_F, lrun = 0.f, b_max = -60.f;
+    float mrun = -CUDART_INF_F, lrun = 0.f, prun = 0.f;      // prun: the sum of P, which bounds O
     {
         unsigned int sr[COLS];
         bool ok_s = false;
@@ -837,7 +830,6 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
             const float muse = (mnew == -CUDART_INF_F) ? 0.f : mnew;
             const float corr = ex2_approx(mrun - muse);
             mrun = mnew;
-            b_max = fmaxf(b_max, eb.x);
             const float2 sc2 = make_float2(row_scale, row_scale), nm2 = make_float2(eb.x - muse + PG_LIFT, eb.x - muse + PG_LIFT);
             float2 ls0 = make_float2(0.f, 0.f), ls1 = make_float2(0.f, 0.f);
             uint4 pk[COLS / 8];
@@ -858,6 +850,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 pk[c8].z = pg_pack_half(pv[2].x, pv[2].y); pk[c8].w = pg_pack_half(pv[3].x, pv[3].y);
             }
             const float2 ls = add2_ftz(ls0, ls1);
+            prun = fmaf(prun, corr, ls.x + ls.y);
             lrun = fmaf(lrun, corr, (ls.x + ls.y) * eb.y);
             if (n >= 1) {
                 if (!ok_o) mbar_wait(bar_o + half * 8, (unsigned int)(n + 1) & 1u, err);
@@ -891,6 +884,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     __syncwarp();                                            // warp-aligned barriers and tensor memory follow
     tc_fence_after_sync();
 
+    float bound = 448.f * prun;                              // of |O|
     // What stayed out of the product of the tree's values joins O of the rows that see it, in the stream and the copy that the key's column went to: x 2^(t - R), the score t once
     // more from the rows themselves.  Rare, and small code.
     if (nt > 0 && (s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3]) != 0u && (WIDE || half < nt)) {
@@ -923,6 +917,11 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                         if (!(fabsf(x) < 1048576.f)) ov[c] = __float_as_uint(__uint_as_float(ov[c]) + (fabsf(x) < __uint_as_float(PG_ENDLESS) ? weight * x : x * CUDART_INF_F));
                     }
                 }
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    const float o = fabsf(__uint_as_float(ov[c]));
+                    if (o < CUDART_INF_F) bound = fmaxf(bound, o);
+                }
                 __syncwarp();
                 tmem_st16(at, ov);
             }
@@ -935,10 +934,10 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     if (!WIDE) {
         float* s_mx = reinterpret_cast<float*>(gen + Y::x);
         float* s_lx = s_mx + 2 * PG_BM;
-        float* s_bx = s_lx + 2 * PG_BM;
+        float* s_px = reinterpret_cast<float*>(gen + Y::part);       // (the tiles of who has a row are done with)
         s_mx[half * PG_BM + lane_row] = mrun;
         s_lx[half * PG_BM + lane_row] = lrun;
-        if (lane_row == 0) s_bx[half] = b_max;
+        if (act) s_px[half * PG_BM + lane_row] = bound;
         named_bar_sync(1, PG_SM_THREADS);
         tc_fence_after_sync();
         mrun = -CUDART_INF_F;
@@ -948,13 +947,18 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
         w0 = ex2_approx(s_mx[lane_row] - muse);
         w1 = ex2_approx(s_mx[PG_BM + lane_row] - muse);
         lrun = 0.f;
+        bound = 0.f;
 #pragma unroll
-        for (int k = 0; k < 2 * REP; ++k) lrun += s_lx[k * (REP > 1 ? ROWS : PG_BM) + row] * ex2_approx(s_mx[k * (REP > 1 ? ROWS : PG_BM) + row] - muse);
-        b_max = fmaxf(s_bx[0], s_bx[1]);
+        for (int k = 0; k < 2 * REP; ++k) {
+            const int at = k * (REP > 1 ? ROWS : PG_BM) + row;
+            const float w = ex2_approx(s_mx[at] - muse);
+            lrun = fmaf(s_lx[at], w, lrun);
+            bound = fmaf(s_px[at], w, bound);
+        }
     }
-    // (a row that sees values from outside the product has them in its partial)
-    if (s_apart != 0u && ((mk0 & (s_odd[0] | (unsigned long long)s_odd[1] << 32)) | (mk1 & (s_odd[2] | (unsigned long long)s_odd[3] << 32))) != 0ull)
-        b_max = fmaxf(b_max, (float)((int)(s_apart >> 23) - 127 - 8));
+    // The row's O is sent as f16 times 2^-k, with its largest possible value in [2^14, 2^15): a value keeps its eleven bits down to 2^-28 of that, and loses nothing to other rows, or
+    // to what this one weighs with nothing.
+    const float kx = (float)max((int)(__float_as_uint(fmaxf(bound, 0.f)) >> 23) - 127 - 14, 0);
     // 16 columns of the row's O; up to 128 rows: of the thread's half of the columns, both streams (a stream without tiles has no O)
     constexpr int CH = WIDE ? 8 : 4;
     const int col_base = WIDE ? 0 : half * 64;
@@ -979,14 +983,14 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     const float inv = lrun > 0.f ? rcp_approx(lrun) : 0.f;
     // fewer rows than 128: the copies' partials meet in shared memory; items of (row, 8 columns) follow instead of rows
     float* s_part = reinterpret_cast<float*>(gen + Y::part);
-    float* s_fin = reinterpret_cast<float*>(gen + Y::x);     // by row: max, sum, 1 / sum, B (over the streams' maxima and sums, which all threads have read)
+    float* s_fin = reinterpret_cast<float*>(gen + Y::x);     // by row: max, sum, 1 / sum, k (over the streams' maxima and sums, which all threads have read)
     if constexpr (REP > 1) {
         named_bar_sync(1, PG_SM_THREADS);
         if (copy == 0 && half == 0) {
             s_fin[row] = mrun;
             s_fin[PG_BM + row] = lrun;
             s_fin[2 * PG_BM + row] = inv;
-            s_fin[3 * PG_BM + row] = b_max;
+            s_fin[3 * PG_BM + row] = kx;
         }
 #pragma unroll 1
         for (int ch = 0; ch < CH; ++ch) {
@@ -1055,9 +1059,8 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
         }
         if (orow >= 0 && p.lse_out && (WIDE || half == 0)) p.lse_out[orow] = (mrun - PG_LIFT + log2f(lrun)) * LN2;
     } else {
-        // Row rl of the block's live ones is merged by CTA rl * ns / live.  Every thread sends its part of its row, {O / l / 2^B in f16, max, sum, B}, from registers into the owner's
-        // receive area by asynchronous stores that complete on the owner's barrier.  (A normalised partial is a convex combination of values below 448 * 2^B:
-        // f16 keeps it to 2^-12.)  A sender may leave at once.
+        // Row rl of the block's live ones is merged by CTA rl * ns / live.  Every thread sends its part of its row, {O 2^-k in f16, max, sum, k}, from registers into the owner's
+        // receive area by asynchronous stores that complete on the owner's barrier.  A sender may leave at once.
         const unsigned char* po = gen + Y::recv;
         const unsigned int s_recv = base + Y::recv;
         const int rows_max = (live + ns - 1) / ns + 1;
@@ -1069,10 +1072,10 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 const int owner = rl * ns / live, o_lo = (owner * live + ns - 1) / ns;
                 const unsigned int dst = cluster_map_addr(s_recv + (unsigned int)(split * rows_max + rl - o_lo) * PG_ROW_STRIDE, owner);
                 const unsigned int rbar = cluster_map_addr(bar_r, owner);
-                const float B = s_fin[3 * PG_BM + rl], f = s_fin[2 * PG_BM + rl] * power_of_two(-(int)B);
+                const float k = s_fin[3 * PG_BM + rl], f = power_of_two(-(int)k);
                 float v[8];
                 part8(rl, c8, v);
-                if (c8 == 0) st_async_v4(dst + HS_HEAD_DIM * 2, __float_as_uint(s_fin[rl]), __float_as_uint(s_fin[PG_BM + rl]), __float_as_uint(B), 0u, rbar);
+                if (c8 == 0) st_async_v4(dst + HS_HEAD_DIM * 2, __float_as_uint(s_fin[rl]), __float_as_uint(s_fin[PG_BM + rl]), __float_as_uint(k), 0u, rbar);
                 st_async_v4(dst + c8 * 16, pg_pack_half(v[0] * f, v[1] * f), pg_pack_half(v[2] * f, v[3] * f), pg_pack_half(v[4] * f, v[5] * f), pg_pack_half(v[6] * f, v[7] * f), rbar);
             }
         } else if (act) {
@@ -1082,8 +1085,8 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
             const unsigned int dst = cluster_map_addr(s_recv + (unsigned int)(split * rows_max + rb - o_lo) * PG_ROW_STRIDE, owner);
             const unsigned int rbar = cluster_map_addr(bar_r, owner);
             if (send && (WIDE || half == 0))
-                st_async_v4(dst + HS_HEAD_DIM * 2, __float_as_uint(mrun), __float_as_uint(lrun), __float_as_uint(b_max), 0u, rbar);
-            const float f = inv * power_of_two(-(int)b_max);
+                st_async_v4(dst + HS_HEAD_DIM * 2, __float_as_uint(mrun), __float_as_uint(lrun), __float_as_uint(kx), 0u, rbar);
+            const float f = power_of_two(-(int)kx);
 #pragma unroll 1
             for (int ch = 0; ch < CH; ++ch) {
                 float ov[16];
@@ -1105,8 +1108,8 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) Mx = fmaxf(Mx, __shfl_xor_sync(HS_FULL_MASK, Mx, o));
             // (a sum that is NaN stays one, also where no score was a number)
-            float w = t.x == -CUDART_INF_F && !(t.y != t.y) ? 0.f : ex2_approx(t.x - Mx) * t.y;
-            float lsum = w;
+            float w = t.x == -CUDART_INF_F && !(t.y != t.y) ? 0.f : ex2_approx(t.x - Mx);
+            float lsum = w * t.y;
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) lsum += __shfl_xor_sync(HS_FULL_MASK, lsum, o);
             w *= (lsum > 0.f ? rcp_approx(lsum) : lsum) * power_of_two((int)t.z);

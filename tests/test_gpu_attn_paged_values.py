@@ -1,0 +1,110 @@
+"""hs_tree_verify_attention_paged where values of very different sizes meet: in tokens of one tile, in tiles of one split, in splits, in nodes that a row's mask hides.  What a row
+loses is bounded by what it weighs itself: 2^-24 of its largest product of a weight and that token's largest value, for every key."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+from paged_route import route
+from paged_util import attention64, i32, make_trees, masks
+from paper_2505_13254_b200 import binding as hb
+
+pytestmark = pytest.mark.gpu
+
+LOG2 = math.log(2.0)
+SCALE = 128 ** -0.5
+
+
+def shared_cache(batch, K, V, page=64):
+    """(cache, K, V as the cache holds them): every sequence has the same tokens [n, hkv, 128], in the same pages."""
+    n, hkv = K.shape[:2]
+    pages = max(1, -(-n // page))
+    pools = []
+    for x in (K, V):
+        byte, scale = paged.quantise(x)
+        pad = pages * page - n
+        byte, scale = np.concatenate([byte, np.full((pad, hkv, 128), 127, np.uint8)]), np.concatenate([scale, np.full((pad, hkv), 255, np.uint8)])
+        pools.append((byte.reshape(pages, page, hkv, 128).transpose(0, 2, 1, 3), scale.reshape(pages, page, hkv).transpose(0, 2, 1)))
+    t = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    cache = hb.KvCache(t(pools[0][0]), t(pools[1][0]), t(pools[0][1]), t(pools[1][1]), i32([list(range(pages))] * batch), i32([n] * batch))
+    return cache, paged.dequantise(*paged.quantise(K)), paged.dequantise(*paged.quantise(V))
+
+
+def check(out, lse, q, K, V, kt, vt, mask, apart=True):
+    """The bound, term by term: the bf16 output, half a step of 2^-8; P in f16 and the partials of splits in f16, 2^-11 of the weighted mean of |v| each; scores off by delta change a
+    weight by e^delta - 1, and the sum as much, with what fp32 sums and ex2 add, 2^-16; of every key 2^-24 of the row's largest product of a weight and its token's largest value.  Tree values of 2^10 and more are apart: their
+    token counts as 2^11 there, and the partials keep 2^-38 of such a product."""
+    d = lambda a: torch.as_tensor(np.asarray(a), dtype=torch.float64, device="cuda") if not torch.is_tensor(a) else a.double()
+    want, want_lse, mean, delta, _ = attention64(q, K, V, kt, vt, mask, SCALE)
+    G, n, cached = q.shape[1] // kt.shape[1], len(q), len(K)
+    vis = torch.cat([torch.ones(n, cached, dtype=torch.bool, device="cuda"), torch.as_tensor(mask, device="cuda")], 1)
+    s = torch.einsum("nhd,khd->hnk", d(q), torch.cat([d(K), d(kt)]).repeat_interleave(G, 1)) * SCALE
+    w = torch.softmax(s.masked_fill(~vis, -math.inf), 2).masked_fill(~vis, 0)
+    size, tree = d(V).abs().amax(2), d(vt).abs().amax(2)
+    ordinary = torch.cat([size, torch.where(tree >= 2.0 ** 10, 2.0 ** 11, tree)]).repeat_interleave(G, 1).T[:, None]
+    top, far = (w * ordinary).amax(2).T, (w * torch.cat([size, tree]).repeat_interleave(G, 1).T[:, None]).amax(2).T
+    e = delta[:, :, None]
+    bound = 2.0 ** -8 * want.abs() + (2 * 2.0 ** -11 + 2 * torch.expm1(e) + 2.0 ** -16) * mean * (1 + 2.0 ** -8)
+    bound += (vis.sum(1)[:, None] * 2.0 ** -24 * top + 2.0 ** -38 * far)[:, :, None]
+    err = (out.double() - want).abs()
+    assert not torch.isnan(out).any()
+    assert (err <= bound).all(), float((err / bound.clamp_min(1e-300)).max())
+    assert ((lse.double() - want_lse).abs() <= delta + 2.0 ** -18 + 2.0 ** -22 * want_lse.abs()).all()
+
+
+def run(ctx, pr, cache, q, k, v, nodes):
+    lse = torch.zeros(q.shape[:2], device="cuda")
+    out = hb.hs_tree_verify_attention_paged(ctx, pr, cache, q, k, v, max_nodes=max(nodes), max_kv_len=int(cache.kv_len.max()), lse_out=lse)
+    assert hb.hs_device_error(ctx) == 0
+    return out, lse
+
+
+def hide(pr, first, nodes, hidden):
+    """Node `hidden` of every tree is seen by its own row only."""
+    words = pr.anc_mask.clone()
+    for f, n in zip(first, nodes):
+        own = words[f + hidden].clone()
+        words[f:f + n, hidden >> 6] &= ~(1 << (hidden & 63))
+        words[f + hidden] = own
+    pr.anc_mask.copy_(words)
+
+
+SHAPES = [  # batch, nodes, hq, hkv, tokens, (rows of a block, splits)
+    (1, 5, 4, 1, 3000, (32, 16)), (1, 7, 16, 2, 3000, (64, 16)), (1, 60, 8, 2, 3000, (128, 16)), (10, 60, 32, 8, 4096, (256, 3)), (19, 5, 32, 8, 1000, (32, 1)),
+    (16, 60, 32, 8, 300, (256, 1)),
+]
+
+
+def random_case(batch, nodes, hq, hkv, tokens, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rng = np.random.default_rng(seed)
+    cache, K, V = shared_cache(batch, rng.standard_normal((tokens, hkv, 128)), rng.standard_normal((tokens, hkv, 128)))
+    ctx, _, pr = make_trees([nodes] * batch, seed)
+    rn = lambda h: torch.randn(batch * nodes, h, 128, device="cuda", generator=g).bfloat16()
+    return ctx, pr, cache, K, V, rn(hq), rn(hkv), rn(hkv)
+
+
+@pytest.mark.parametrize("other", [2.0 ** 40, -2.0 ** 90, 2.0 ** 99])
+@pytest.mark.parametrize("batch, nodes, hq, hkv, tokens, how", SHAPES)
+def test_a_huge_value_costs_the_rows_that_mask_it_nothing_whatever_they_see(batch, nodes, hq, hkv, tokens, how, other):
+    """Nodes 2 and 3 are seen by their own rows only; the rows of 2 see 2^20 beside a sibling that is larger by far."""
+    assert route(batch, nodes, hq, hkv, tokens) == how
+    ctx, pr, cache, K, V, q, k, v = random_case(batch, nodes, hq, hkv, tokens, 31)
+    first = [b * nodes for b in range(batch)]
+    hide(pr, first, [nodes] * batch, 2)
+    hide(pr, first, [nodes] * batch, 3)
+    words = pr.anc_mask.clone()
+    for f in first:
+        words[f + 2, 0] &= ~8
+        words[f + 3, 0] &= ~4
+        v[f + 2, :, 5], v[f + 3, :, 7] = 2.0 ** 20, other
+    pr.anc_mask.copy_(words)
+    out, lse = run(ctx, pr, cache, q, k, v, [nodes] * batch)
+    for b, m in list(enumerate(masks(pr, [nodes] * batch)))[::7]:
+        r, rows = slice(first[b], first[b] + nodes), [i for i in range(nodes) if i != 3]
+        small = v[r].clone()
+        small[3] = 0                                                     # (seen by none of the rows that are looked at)
+        check(out[r][rows], lse[r][rows], q[r][rows], K, V, k[r], small, m[rows])
+    ctx.close()
