@@ -413,10 +413,11 @@ typedef struct {
  * A row that sees nothing gives 0 with lse_out = -inf; rows that belong to no kept node are left as they were.  A tree of more nodes
  * than max_nodes, or with rows (ORIGINAL: of the drafted tree) from max_rows on, is left out, with HS_ERR_SHAPE in the error word.
  * Numerics: queries and tree keys enter the scores as two E4M3 terms, which hold a bf16 value exactly down to 2^-9 of the largest of
- * its row and smaller ones to within 2^-17 of that one; cached keys enter as they are, sums are fp32.  The weights and the values are f16 in the product,
- * the values relative to the largest one of their tile (64 tokens of the prefix, or 64 kept nodes): bits below 2^-33 of that are lost, and values below
- * 2^-84 count as zero.  Tree values of 2^20 and more, and those that are not finite, stay out of that: they reach the rows that see them, in fp32 (from 2^100
- * on as infinities), and no other; beside them such a row keeps its other values to 2^-38 of them.  A query, a tree key or a cached row with a value that is not finite makes NaN of the rows that see it.
+ * its row and smaller ones to within 2^-17 of that one; cached keys enter as they are, sums are fp32.  The weights and the values are f16 in the
+ * product, the weights to 2^-11 of themselves, every key's share down to 2^-24 of the row's largest product of a weight and its token's largest |value|
+ * (what a row masks or weighs with next to nothing costs it nothing), a tree value down to 2^-26 of its token's largest; values below 2^-84 count as zero.  Tree values of
+ * 2^10 and more, and those that are not finite, stay out of that: they reach the rows that see them, in fp32 (from 2^100 on as infinities), and no other.  Where the keys
+ * are split, a row's partial sums are f16 too, to 2^-11 of themselves, or 2^-38 of the largest product there.  A query, a tree key or a cached row with a value that is not finite makes NaN of the rows that see it.
  * n_pages * hkv * page_size <= 2^31 - 1, batch * hkv <= 65535. */
 hs_status hs_tree_verify_attention_paged(hs_ctx* ctx, const hs_pruned_tree* pruned, const hs_kv_cache* cache,
                                          const hs_paged_attn_desc* desc, const void* q, const void* k_tree,

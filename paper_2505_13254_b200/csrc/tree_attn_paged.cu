@@ -11,10 +11,11 @@
 // 2^9 below it or more is rounded to 2^-9, by at most 2^-17 of that value.  The keys' scales, powers of two, multiply the columns of S.  The tree's bf16 keys become
 // two terms in the same way, and their S four products.
 // O = P V has no such form: probabilities span more than eight bits can hold (a thousand keys of weight 2^-18 beside one of weight 1 matter).  So V's bytes become f16
-// tiles in shared memory, exactly, and P is rounded to f16, eleven bits, all that is rounded on the way.  A tile's rows carry their scale relative to the tile's
-// largest, 2^B, which goes into the exponential's argument: P = 2^(t + B - R) with t the score in base 2 and R the running maximum of t + B, so that O += P V' holds
-// 2^-R sum 2^t V whatever the tiles' scales are, and the sum takes P 2^-B.  A row 2^15 below its tile's largest begins to lose low bits; they are 2^-33 of
-// the largest value.
+// tiles in shared memory, exactly, and P is rounded to f16, eleven bits, all that is rounded on the way.  The values' scales go into the exponential's argument:
+// P = 2^(t + B - R) with t the score in base 2, 2^B the token's scale and R the running maximum of t + B, so that O += P V' holds 2^-R sum 2^t V whatever the scales are, and the
+// sum takes P 2^-B.  R follows what a row weighs, not what it masks or weighs with nothing: f16 keeps products of a weight and a token's values down to 2^-30 of the row's largest.
+// Where the scales of a tile's tokens lie within 2^6 of one another, all of them take the largest (V' then carries the difference, exactly), B is one number a tile and goes into the
+// exponential's multiply-add for nothing; that costs the bound 2^6.  Other tiles (rare in earnest: a token of next to no value among others) take a term, and an exponential for the sum, a score more.
 //   - two warps ask for keys (TMA, a page at a time, 128-byte swizzle: operand tiles)
 //   - eight warps in four groups ask for the values and the scale bytes of every fourth tile (bulk copies) and turn the values into a swizzled f16 tile: four bytes by two PRMT, shifts and masks, one product a pair with the row's
 //     power of two; and the keys' scale bytes into floats
@@ -29,8 +30,8 @@
 // 4.0 TB/s with both CTAs' starts and ends; a CTA spends 12000 clocks on those).  Trees behind long prefixes: the softmax warps' instructions (four trees of 62 nodes and 64 heads behind
 // 32768 tokens, 267 GFLOP: 355 us, 0.75 PFLOP/s; an SM issues in 59% of its clocks, the exponential unit is busy in 44%, the products take 512 of a tile's 1300 clocks).  Small calls: the
 // chain from the launch to the merged rows (one token behind 512: 7.7 us; a tree of 60 behind 2048: 16.5 us).
-// Behind the last token and in the last page a tile is zero, whatever the memory holds, and masked.  A tree value that is not finite, or of 2^20 and more, is
-// zero in the product (0 * inf would reach the rows that mask it, and a huge one would cost its tile's others their bits) and added to the rows that see it at the end.
+// Behind the last token and in the last page a tile is zero, whatever the memory holds, and masked.  A tree value that is not finite, or of 2^10 and more, is
+// zero in the product (0 * inf would reach the rows that mask it, and a large one would cost the other columns of the rows that see it their bits) and added to the rows that see it at the end.
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
@@ -49,6 +50,7 @@
 #define PG_KEYS 6                                   // tiles of K (a tree tile is two: its terms)
 #define PG_GROUPS 4                                 // groups of converters, and f16 tiles of V
 #define PG_EXPS 8                                   // tiles whose scales are kept
+#define PG_FLAT 6                                   // a tile whose tokens' exponents differ by no more has one for all of them
 #define PG_LIFT 6.f                                 // P = 2^(6 + ..): f16 then keeps weights down to 2^-30 of the largest
 #define PG_ROW_STRIDE (HS_HEAD_DIM * 2 + 16)        // a pushed partial row: 128 f16 of O 2^-k, {max, sum, k}
 #define PG_THREADS 640
@@ -78,11 +80,12 @@ struct Layout {
     static constexpr int scale = q + (!WIDE && recv_bytes > q_bytes ? recv_bytes : q_bytes);      // scale bytes of the units: V's 64, K's 64
     static constexpr int bar = scale + units * 2 * PG_BN;
     static constexpr int x = bar + 512;              // the streams' maxima and sums, [2][128] each
-    static constexpr int exps = x + 4 * PG_BM * 4;   // per tile {B, 2^-B}
+    static constexpr int exps = x + 4 * PG_BM * 4;   // per tile {B, 2^-B}, {0, 0} where the tokens have exponents of their own
     static constexpr int ks = exps + 2 * PG_EXPS * 4;     // per tile the keys' scales
-    static constexpr int qs = ks + PG_EXPS * PG_BN * 4;   // the query rows' scales
-    static constexpr int red = qs + rows * 4;             // maxima of the softmax warps
-    static constexpr int end = red + 32;
+    static constexpr int vs = ks + PG_EXPS * PG_BN * 4;   // and the tokens' exponents
+    static constexpr int qs = vs + PG_EXPS * PG_BN;       // the query rows' scales
+    static constexpr int red = qs + rows * 4;             // largest and smallest exponents of the converting warps
+    static constexpr int end = red + 64;
     static constexpr int part = k;                   // fewer rows than 128: the streams' partials, 128 rows of part_stride floats
     static constexpr int part_stride = HS_HEAD_DIM + 4;
     static_assert(PG_BM * part_stride * 4 <= q, "they lie over the tiles");
@@ -157,14 +160,23 @@ __device__ __forceinline__ float rcp_approx(float x) {
 __device__ __forceinline__ void copy16(unsigned int dst, const void* src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
 }
-// The reference exponent of a tile whose largest scale byte (or that of its largest |x|) is s: at least -60, so that sums of P 2^-B stay far inside fp32.
-__device__ __forceinline__ int tile_exponent(unsigned int s) { return max((int)s - 127, -60); }
+// The exponent of a token whose scale byte (or that of its largest |x|) is s: at least -60, so that sums of P 2^-B stay far inside fp32.
+#define PG_SMALLEST 67u
+__device__ __forceinline__ int token_exponent(unsigned int s) { return (int)max(s, PG_SMALLEST) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((unsigned int)(e + 127) << 23); }
 // bits of the larger |.| of a pair of bf16, as fp32
 __device__ __forceinline__ unsigned int pair_amax(unsigned int w) { return max(w << 16 & 0x7fff0000u, w & 0x7fff0000u); }
-// A tree value of 2^20 or more, an infinity or a NaN stays out of the product: what it would cost the f16 values beside it, or put into rows that mask it, it is added
+__device__ __forceinline__ unsigned int pair_max(unsigned int a, unsigned int b) {
+    asm("max.u16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return a;
+}
+__device__ __forceinline__ unsigned int pair_min(unsigned int a, unsigned int b) {
+    asm("min.u16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return a;
+}
+// A tree value of 2^10 or more, an infinity or a NaN stays out of the product: what it would cost the other columns, or put into rows that mask it, it is added
 // to the rows that see it at the end.  A pair without such values:
-#define PG_APART 0x49800000u                        // 2^20, the bits
+#define PG_APART 0x44800000u                        // 2^10, the bits
 #define PG_ENDLESS 0x71800000u                      // 2^100: weights of up to 2^14 times more would leave fp32, it counts as infinite
 __device__ __forceinline__ unsigned int near_or_zero(unsigned int w) {
     return ((w << 16 & 0x7fff0000u) >= PG_APART ? 0u : w & 0xffffu) | ((w & 0x7fff0000u) >= PG_APART ? 0u : w & 0xffff0000u);
@@ -322,6 +334,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     const int warp_u = __shfl_sync(HS_FULL_MASK, warp, 0);
     float2* s_B = reinterpret_cast<float2*>(gen + Y::exps);             // {B, 2^-B} of tile i at i % PG_EXPS
     float* s_ks = reinterpret_cast<float*>(gen + Y::ks);                // its keys' scales
+    signed char* s_vs = reinterpret_cast<signed char*>(gen + Y::vs);    // its tokens' exponents
     unsigned int* s_red = reinterpret_cast<unsigned int*>(gen + Y::red);
 
     // A row of 128 bf16 in two halves of a tile becomes its two terms, 128 bytes each, in their place, by the sixteen lanes that brought it, and 2^e in out[]: NaN where
@@ -330,7 +343,8 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     // (a tree of 60 behind 100 tokens 11.5, with one 12.0).
     constexpr int TERM_ROWS = REP > 1 ? 1 : 4;
     const int sub = tid & 15;
-    auto to_terms = [&](unsigned char* tile, int half_bytes, int first, int rows, float* out) {
+    // also: scale bytes of other rows, two by two, of which the sixteen lanes find the largest on the way.
+    auto to_terms = [&](unsigned char* tile, int half_bytes, int first, int rows, float* out, auto&... also) {
         uint4 w[TERM_ROWS];
         unsigned int a[TERM_ROWS];
 #pragma unroll
@@ -343,6 +357,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
         for (int o = 8; o > 0; o >>= 1) {
 #pragma unroll
             for (int j = 0; j < TERM_ROWS; ++j) a[j] = max(a[j], __shfl_xor_sync(HS_FULL_MASK, a[j], o));
+            ((also = pair_max(also, __shfl_xor_sync(HS_FULL_MASK, also, o))), ...);
         }                                                // (and every lane has read its part of the rows)
 #pragma unroll
         for (int j = 0; j < TERM_ROWS; ++j) {
@@ -445,17 +460,18 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();                                    // (rows are read by other lanes than those that brought them)
-            // The tree's tiles: keys as terms; values as f16 relative to the largest that is finite, what is not leaves them.
+            // The tree's tiles: keys as terms; values as f16 relative to their exponents, without those that stay apart.
 #pragma unroll 1
             for (int t = 0; t < nt; ++t) {
                 unsigned char* tile = gen + Y::v + t * PG_TILE_BYTES;
-                unsigned int a = 0u;
-                const int keys16 = min(PG_BN, (nk - (g0 + t) * PG_BN + 15) & ~15);       // (those behind them are masked, and zeros)
+                unsigned int hi = 0u, lo = 255u;             // of the live tokens' scale bytes
+                const int live_keys = nk - (g0 + t) * PG_BN, keys16 = min(PG_BN, (live_keys + 15) & ~15);       // (those behind them are masked, and zeros)
                 [[maybe_unused]] uint4 v[PG_BN / 16];
+                [[maybe_unused]] unsigned int pair[PG_BN / 32];              // scale bytes of two rows
+                auto scale_of = [&](int j) { return pair[j >> 1] >> (j & 1) * 16 & 255u; };
                 if constexpr (REP > 1) {                     // a row at a time, read again below
 #pragma unroll 1
                     for (int row = ct8 >> 4; row < keys16; row += 16) {
-                        to_terms(gen + Y::k + t * 2 * PG_UNIT_BYTES, PG_UNIT_BYTES, row, keys16, s_ks + t * PG_BN);
                         uint4* at = reinterpret_cast<uint4*>(tile + pg_off(PG_BN, row, sub));
                         uint4 x = *at;
                         unsigned int m = max(max(pair_amax(x.x), pair_amax(x.y)), max(pair_amax(x.z), pair_amax(x.w)));
@@ -467,10 +483,18 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                             atomicOr(&s_odd[key >> 5], 1u << (key & 31));
                         }
                         __syncwarp();
-                        a = max(a, m);
+                        unsigned int scale = e8m0_of(m);
+                        to_terms(gen + Y::k + t * 2 * PG_UNIT_BYTES, PG_UNIT_BYTES, row, keys16, s_ks + t * PG_BN, scale);
+                        scale = max(scale, PG_SMALLEST);
+                        if (sub == 0) s_vs[t * PG_BN + row] = (signed char)(scale - 127u);
+                        if (row < live_keys) {
+                            hi = max(hi, scale);
+                            lo = min(lo, scale);
+                        }
                     }
                 } else {
                     to_terms(gen + Y::k + t * 2 * PG_UNIT_BYTES, PG_UNIT_BYTES, ct8 >> 4, keys16, s_ks + t * PG_BN);
+                    unsigned int behind[PG_BN / 32];                             // 255 in the place of rows behind the last
 #pragma unroll
                     for (int j = 0; j < PG_BN / 16; ++j) {
                         const int row = (ct8 >> 4) + 16 * j;
@@ -482,30 +506,54 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                             const int key = (g0 + t) * PG_BN + row;
                             atomicOr(&s_odd[key >> 5], 1u << (key & 31));
                         }
-                        a = max(a, m);
+                        const unsigned int none = row < live_keys ? 0u : 255u;
+                        pair[j >> 1] = j & 1 ? pair[j >> 1] | e8m0_of(m) << 16 : e8m0_of(m);
+                        behind[j >> 1] = j & 1 ? behind[j >> 1] | none << 16 : none;
                     }
+                    __syncwarp();
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) {
+#pragma unroll
+                        for (int j = 0; j < PG_BN / 32; ++j) pair[j] = pair_max(pair[j], __shfl_xor_sync(HS_FULL_MASK, pair[j], o));
+                    }
+                    unsigned int h2 = 0u, l2 = 0x00ff00ffu;
+#pragma unroll
+                    for (int j = 0; j < PG_BN / 32; ++j) {
+                        pair[j] = pair_max(pair[j], PG_SMALLEST * 0x10001u);
+                        h2 = pair_max(h2, pair[j]);                              // (rows behind the last are the smallest)
+                        l2 = pair_min(l2, pair[j] | behind[j]);
+                    }
+                    hi = max(h2 & 255u, h2 >> 16);
+                    lo = min(l2 & 255u, l2 >> 16);
                 }
-                a = __reduce_max_sync(HS_FULL_MASK, a);
-                if (lane == 0) s_red[warp - 8] = a;
+                hi = __reduce_max_sync(HS_FULL_MASK, hi);
+                lo = __reduce_min_sync(HS_FULL_MASK, lo);
+                if (lane < 2) s_red[warp - 8 + 8 * lane] = lane ? lo : hi;
                 named_bar_sync(4, PG_SM_THREADS);
-                const int e = tile_exponent(e8m0_of(__reduce_max_sync(HS_FULL_MASK, s_red[lane & 7])));
-                const float f = power_of_two(-e);
+                const unsigned int red = s_red[lane & 15];
+                hi = __reduce_max_sync(HS_FULL_MASK, lane & 8 ? 0u : red);
+                lo = __reduce_min_sync(HS_FULL_MASK, lane & 8 ? red : 255u);
+                const bool flat = hi <= lo + PG_FLAT;
                 if constexpr (REP > 1) {
 #pragma unroll 1
                     for (int row = ct8 >> 4; row < keys16; row += 16) {
                         uint4* at = reinterpret_cast<uint4*>(tile + pg_off(PG_BN, row, sub));
                         const uint4 x = *at;
+                        const float f = power_of_two(flat ? 127 - (int)hi : -s_vs[t * PG_BN + row]);
                         *at = make_uint4(scaled_half2(x.x, f), scaled_half2(x.y, f), scaled_half2(x.z, f), scaled_half2(x.w, f));
                     }
                 } else {
+                    if (flat) pair[0] = pair[1] = hi * 0x10001u;
 #pragma unroll
                     for (int j = 0; j < PG_BN / 16; ++j) {
                         const int row = (ct8 >> 4) + 16 * j;
+                        const float f = power_of_two(127 - (int)scale_of(j));
+                        if (!flat && sub == 0) s_vs[t * PG_BN + row] = (signed char)(scale_of(j) - 127u);
                         if (row < keys16)
                             *reinterpret_cast<uint4*>(tile + pg_off(PG_BN, row, sub)) = make_uint4(scaled_half2(v[j].x, f), scaled_half2(v[j].y, f), scaled_half2(v[j].z, f), scaled_half2(v[j].w, f));
                     }
                 }
-                if (ct8 == 0) s_B[t] = make_float2((float)e, power_of_two(-e));
+                if (ct8 == 0) s_B[t] = flat ? make_float2((float)((int)hi - 127), power_of_two(127 - (int)hi)) : make_float2(0.f, 0.f);
                 fence_proxy_async_smem();
                 named_bar_sync(4, PG_SM_THREADS);
                 // what the loader and a group would bring to the tile's barriers
@@ -536,12 +584,16 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 bool back = true;                            // the tile's place is free
                 if (i >= PG_GROUPS) back = mbar_test_wait(bar_ev + slot * 8, back_phase);
                 const unsigned int sa = two & 255u, sb = two >> 8;
-                const unsigned int top = __reduce_max_sync(HS_FULL_MASK, max(2 * lane < left && sa != 255u ? sa : 0u, 2 * lane + 1 < left && sb != 255u ? sb : 0u));
-                const int e = tile_exponent(top);
+                const bool la = 2 * lane < left && sa != 255u, lb = 2 * lane + 1 < left && sb != 255u;      // (a token of no number has no size)
+                const int hi = token_exponent(__reduce_max_sync(HS_FULL_MASK, max(la ? sa : 0u, lb ? sb : 0u)));
+                const int lo = token_exponent(__reduce_min_sync(HS_FULL_MASK, min(la ? sa : 255u, lb ? sb : 255u)));
+                const bool flat = hi - lo <= PG_FLAT;
+                const int e = flat ? hi : token_exponent(s);
                 // The tile's scales, ahead of S.  (Their places were last used eight tiles back, by a P V that this group has waited for.)  A row of scale byte 255 is NaN
                 // whatever its bytes are.
                 s_ks[(i & (PG_EXPS - 1)) * PG_BN + key] = __uint_as_float(s_key == 255u ? 0x7fffffffu : s_key << 23);
-                if (ct == 0) s_B[i & (PG_EXPS - 1)] = make_float2((float)e, power_of_two(-e));
+                if (ct == 0) s_B[i & (PG_EXPS - 1)] = flat ? make_float2((float)hi, power_of_two(-hi)) : make_float2(0.f, 0.f);
+                if (!flat) s_vs[(i & (PG_EXPS - 1)) * PG_BN + key] = (signed char)min(e, 127);
                 mbar_arrive(bar_x + (i & (PG_EXPS - 1)) * 8);
                 // (behind the last key the factor is zero: spread bytes are finite, whatever they were)
                 const unsigned int f = key >= left ? 0u : s == 255 ? 0x7fff7fffu : half2_power(s - 127 - e + 8);
@@ -749,7 +801,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     if (WIDE) fence_proxy_async_smem();                      // (the second block is read by the tensor cores)
     named_bar_sync(1, PG_SM_THREADS);
     float row_scale = p.scale_log2 * s_qs[(WIDE ? half * PG_BM : 0) + row];
-    if (row_scale < 1e-37f) row_scale = 1e-37f;              // (0 * -inf in a masked column would be NaN; a NaN stays)
+    if (row_scale < 1e-35f) row_scale = 1e-35f;              // (0 * -inf in a masked column would be NaN, and a token's exponent over it stays finite; a NaN stays)
     if (!WIDE || half == 0) {
 #pragma unroll 1
         for (int c0 = WIDE ? 0 : half * 8; c0 < (WIDE ? 16 : half * 8 + 8); c0 += 4) {
@@ -776,6 +828,9 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     float mrun = -CUDART_INF_F, lrun = 0.f, prun = 0.f;      // prun: the sum of P, which bounds O
     {
         unsigned int sr[COLS];
+        // The reference of the exponents follows the maximum only when that has grown by more than 8: until then P <= 2^14 instead of <= 2^6, which f16
+        // holds as exactly, and O is rescaled a few times per row instead of whenever any row of the warp sees a new maximum.
+        auto follow = [&](float mx) { return (mx > mrun + 8.f || mrun == -CUDART_INF_F) ? fmaxf(mrun, mx) : mrun; };
         bool ok_s = false;
         int n = 0;                                           // the stream's tiles so far
 #pragma unroll 1
@@ -807,7 +862,8 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
             const bool is_tree = i < nt;
             const int col0 = (is_tree ? g0 + i : g0 + i - tree_tiles) * PG_BN;
             const int nvis = (is_tree ? nk : L) - col0;
-            if (is_tree || nvis < PG_BN) {
+            float sum = 0.f;                                 // of 2^(t - R), where the tile's tokens have exponents of their own
+            if (is_tree || nvis < PG_BN || eb.y == 0.f) {    // (one branch for what is rare: a second one in the chain costs every tile, long trees 380 to 393 us)
                 unsigned long long vis64 = nvis >= 64 ? ~0ull : ((1ull << max(nvis, 0)) - 1ull);
                 if (is_tree) vis64 &= (col0 == 0 ? mk0 : mk1);
                 vis64 >>= copy * COLS;
@@ -815,6 +871,28 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
 #pragma unroll
                 for (int c = 0; c < COLS; ++c)
                     if (!(((c < 32 ? vlo : vhi) >> (c & 31)) & 1u)) sr[c] = __float_as_uint(-CUDART_INF_F);
+                if (eb.y == 0.f) {                           // t + B in place of t
+                    // (volatile: read twice rather than kept, the registers are full)
+                    const volatile unsigned int* vs = reinterpret_cast<const volatile unsigned int*>(s_vs + (i & (PG_EXPS - 1)) * PG_BN + copy * COLS);
+                    const float inv = rcp_approx(row_scale);
+                    float top = -CUDART_INF_F;
+#pragma unroll
+                    for (int c = 0; c < COLS; c += 4) {
+                        const unsigned int w = vs[c >> 2];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            sr[c + e] = __float_as_uint(fmaf((float)(signed char)(w >> e * 8), inv, __uint_as_float(sr[c + e])));
+                            top = fmaxf(top, __uint_as_float(sr[c + e]));
+                        }
+                    }
+                    const float m = follow(top * row_scale), shift = PG_LIFT - (m == -CUDART_INF_F ? 0.f : m);
+#pragma unroll
+                    for (int c = 0; c < COLS; c += 4) {
+                        const unsigned int w = vs[c >> 2];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum += ex2_approx(fmaf(__uint_as_float(sr[c + e]), row_scale, shift) - (float)(signed char)(w >> e * 8));
+                    }
+                }
             }
             float mxa = -CUDART_INF_F, mxb = -CUDART_INF_F;
 #pragma unroll
@@ -824,10 +902,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
             }
             // (the scale is positive: it commutes with the maximum and folds into the exponent's multiply-add)
             const float mx = fmaf(fmaxf(mxa, mxb), row_scale, eb.x);
-            // The reference of the exponents follows the maximum only when that has grown by more than 8: until then P <= 2^14 instead of <= 2^6, which f16
-            // holds as exactly, and O is rescaled a few times per row instead of whenever any row of the warp sees a new maximum.
-            const float mnew = (mx > mrun + 8.f || mrun == -CUDART_INF_F) ? fmaxf(mrun, mx) : mrun;
-            const float muse = (mnew == -CUDART_INF_F) ? 0.f : mnew;
+            const float mnew = follow(mx), muse = (mnew == -CUDART_INF_F) ? 0.f : mnew;
             const float corr = ex2_approx(mrun - muse);
             mrun = mnew;
             const float2 sc2 = make_float2(row_scale, row_scale), nm2 = make_float2(eb.x - muse + PG_LIFT, eb.x - muse + PG_LIFT);
@@ -845,13 +920,13 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 }
                 ls0 = add2_ftz(ls0, add2_ftz(pv[0], pv[1]));
                 ls1 = add2_ftz(ls1, add2_ftz(pv[2], pv[3]));
-                // P in f16, off by at most 2^-12 of itself each; the sum keeps the unrounded values
+                // P in f16, off by at most 2^-11 of itself each; the sum keeps the unrounded values
                 pk[c8].x = pg_pack_half(pv[0].x, pv[0].y); pk[c8].y = pg_pack_half(pv[1].x, pv[1].y);
                 pk[c8].z = pg_pack_half(pv[2].x, pv[2].y); pk[c8].w = pg_pack_half(pv[3].x, pv[3].y);
             }
             const float2 ls = add2_ftz(ls0, ls1);
             prun = fmaf(prun, corr, ls.x + ls.y);
-            lrun = fmaf(lrun, corr, (ls.x + ls.y) * eb.y);
+            lrun = fmaf(lrun, corr, fmaf(ls.x + ls.y, eb.y, sum));
             if (n >= 1) {
                 if (!ok_o) mbar_wait(bar_o + half * 8, (unsigned int)(n + 1) & 1u, err);
                 tc_fence_after_sync();
@@ -914,7 +989,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
                         const float x = __bfloat162float(p.v_tree[kv + ch + c]);
-                        if (!(fabsf(x) < 1048576.f)) ov[c] = __float_as_uint(__uint_as_float(ov[c]) + (fabsf(x) < __uint_as_float(PG_ENDLESS) ? weight * x : x * CUDART_INF_F));
+                        if (!(fabsf(x) < __uint_as_float(PG_APART))) ov[c] = __float_as_uint(__uint_as_float(ov[c]) + (fabsf(x) < __uint_as_float(PG_ENDLESS) ? weight * x : x * CUDART_INF_F));
                     }
                 }
 #pragma unroll

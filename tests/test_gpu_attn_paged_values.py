@@ -21,15 +21,16 @@ def shared_cache(batch, K, V, page=64):
     """(cache, K, V as the cache holds them): every sequence has the same tokens [n, hkv, 128], in the same pages."""
     n, hkv = K.shape[:2]
     pages = max(1, -(-n // page))
-    pools = []
+    pools, held = [], []
     for x in (K, V):
         byte, scale = paged.quantise(x)
+        held.append(paged.dequantise(byte, scale))
         pad = pages * page - n
         byte, scale = np.concatenate([byte, np.full((pad, hkv, 128), 127, np.uint8)]), np.concatenate([scale, np.full((pad, hkv), 255, np.uint8)])
         pools.append((byte.reshape(pages, page, hkv, 128).transpose(0, 2, 1, 3), scale.reshape(pages, page, hkv).transpose(0, 2, 1)))
     t = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
     cache = hb.KvCache(t(pools[0][0]), t(pools[1][0]), t(pools[0][1]), t(pools[1][1]), i32([list(range(pages))] * batch), i32([n] * batch))
-    return cache, paged.dequantise(*paged.quantise(K)), paged.dequantise(*paged.quantise(V))
+    return cache, held[0], held[1]
 
 
 def check(out, lse, q, K, V, kt, vt, mask, apart=True):
@@ -107,4 +108,68 @@ def test_a_huge_value_costs_the_rows_that_mask_it_nothing_whatever_they_see(batc
         small = v[r].clone()
         small[3] = 0                                                     # (seen by none of the rows that are looked at)
         check(out[r][rows], lse[r][rows], q[r][rows], K, V, k[r], small, m[rows])
+    ctx.close()
+
+
+def level_case(batch, nodes, hq, hkv, tokens, gap, V, levels=None, seed=1):
+    """Scores in the hand: queries 1/2 in every place, cached keys `levels` (1) in theirs, the tree's so that their scores lie `gap` binades above a cached one's."""
+    K = np.ones((tokens, hkv, 128)) * (1.0 if levels is None else levels[:, None, None])
+    cache, K, V = shared_cache(batch, K, V)
+    ctx, _, pr = make_trees([nodes] * batch, seed)
+    n = batch * nodes
+    full = lambda h, x: torch.full((n, h, 128), x, device="cuda").bfloat16()
+    return ctx, pr, cache, K, V, full(hq, 0.5), full(hkv, 1.0 + gap * LOG2 / (64 * SCALE)), full(hkv, 1.0)
+
+
+LONG = [(19, 2, 32, 8, 7680, (32, 1)), (19, 12, 32, 8, 7680, (64, 1)), (19, 30, 32, 8, 7680, (128, 1)), (16, 60, 32, 8, 7680, (256, 1)), (1, 60, 32, 8, 7680, (128, 8))]
+
+
+@pytest.mark.parametrize("gap, value", [(13, 1e6), (14, -2.0 ** 19 * 1.9), (14, 1000.0), (12, -50.0)])
+@pytest.mark.parametrize("batch, nodes, hq, hkv, tokens, how", LONG)
+def test_a_hidden_value_costs_the_prefix_nothing(batch, nodes, hq, hkv, tokens, how, gap, value):
+    """A few heavy tree keys before thousands of light cached ones that make up half of the sum."""
+    assert route(batch, nodes, hq, hkv, tokens) == how
+    ctx, pr, cache, K, V, q, k, v = level_case(batch, nodes, hq, hkv, tokens, gap, -np.ones((tokens, hkv, 128)))
+    first = [b * nodes for b in range(batch)]
+    hide(pr, first, [nodes] * batch, 1)
+    for f in first:
+        v[f + 1] = value
+    out, lse = run(ctx, pr, cache, q, k, v, [nodes] * batch)
+    for b, m in list(enumerate(masks(pr, [nodes] * batch)))[::9]:
+        rows, r = [i for i in range(nodes) if i != 1], slice(first[b], first[b] + nodes)
+        check(out[r][rows], lse[r][rows], q[r][rows], K, V, k[r], v[r], m[rows])
+        check(out[r][1:2], lse[r][1:2], q[r][1:2], K, V, k[r], v[r], m[1:2])
+    ctx.close()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 30, -2.0 ** 16, 2.0 ** 90])
+@pytest.mark.parametrize("batch, nodes, hq, hkv, tokens, how", LONG)
+def test_a_cached_value_of_no_weight_costs_nothing(batch, nodes, hq, hkv, tokens, how, size):
+    """One early token of a huge value whose score lies far below the others'."""
+    rng = np.random.default_rng(7)
+    V, levels = rng.uniform(-1.2, -0.8, (tokens, hkv, 128)), rng.choice([0.875, 1.0, 1.125], tokens)
+    V[5], levels[5] = size, -15.0                                       # 16 * 64 / sqrt(128) nats below the others, 2^-130
+    ctx, pr, cache, K, V, q, k, v = level_case(batch, nodes, hq, hkv, tokens, 0, V, levels)
+    out, lse = run(ctx, pr, cache, q, k, v, [nodes] * batch)
+    for b, m in list(enumerate(masks(pr, [nodes] * batch)))[::9]:
+        r = slice(b * nodes, (b + 1) * nodes)
+        check(out[r], lse[r], q[r], K, V, k[r], v[r], m)
+    ctx.close()
+
+
+@pytest.mark.parametrize("spread", [6, 7, 12, 40])
+@pytest.mark.parametrize("batch, nodes, hq, hkv, tokens, how", LONG)
+def test_tokens_of_every_size_weigh_as_they_should(batch, nodes, hq, hkv, tokens, how, spread):
+    """The larger a token's values, the smaller its weight, so that all of them make up the row, in tiles whose sizes differ by 2^spread."""
+    rng = np.random.default_rng(spread)
+    exponent = rng.integers(-(spread // 2), spread - spread // 2 + 1, tokens)
+    V = rng.uniform(0.5, 1.0, (tokens, hkv, 128)) * rng.choice([-1.0, 1.0], (1, hkv, 128)) * 2.0 ** exponent[:, None, None]
+    levels = -exponent * LOG2 / (64 * SCALE)
+    ctx, pr, cache, K, V, q, k, v = level_case(batch, nodes, hq, hkv, tokens, 8, V, levels)
+    g = torch.Generator(device="cuda").manual_seed(spread)
+    v *= torch.exp2(torch.randint(-(spread // 2), min(spread - spread // 2, 9) + 1, (len(v), hkv, 1), device="cuda", generator=g).float()).bfloat16()
+    out, lse = run(ctx, pr, cache, q, k, v, [nodes] * batch)
+    for b, m in list(enumerate(masks(pr, [nodes] * batch)))[::9]:
+        r = slice(b * nodes, (b + 1) * nodes)
+        check(out[r], lse[r], q[r], K, V, k[r], v[r], m)
     ctx.close()
