@@ -416,7 +416,8 @@ typedef struct {
  * its row and smaller ones to within 2^-17 of that one; cached keys enter as they are, sums are fp32.  The weights and the values are f16 in the
  * product, the weights to 2^-11 of themselves, every key's share down to 2^-24 of the row's largest product of a weight and its token's largest |value|
  * (what a row masks or weighs with next to nothing costs it nothing), a tree value down to 2^-26 of its token's largest; values below 2^-84 count as zero.  Tree values of
- * 2^10 and more, and those that are not finite, stay out of that: they reach the rows that see them, in fp32 (from 2^100 on as infinities), and no other.  Where the keys
+ * 2^10 and more, and those that are not finite, stay out of that: they reach the rows that see them, in fp32 (from 2^100 on as infinities), and no other; their
+ * token counts as 2^10 beside the others.  Where the keys
  * are split, a row's partial sums are f16 too, to 2^-11 of themselves, or 2^-38 of the largest product there.  A query, a tree key or a cached row with a value that is not finite makes NaN of the rows that see it.
  * n_pages * hkv * page_size <= 2^31 - 1, batch * hkv <= 65535. */
 hs_status hs_tree_verify_attention_paged(hs_ctx* ctx, const hs_pruned_tree* pruned, const hs_kv_cache* cache,

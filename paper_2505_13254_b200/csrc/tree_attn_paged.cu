@@ -175,9 +175,9 @@ __device__ __forceinline__ unsigned int pair_min(unsigned int a, unsigned int b)
     return a;
 }
 // A tree value of 2^10 or more, an infinity or a NaN stays out of the product: what it would cost the other columns, or put into rows that mask it, it is added
-// to the rows that see it at the end.  A pair without such values:
+// to the rows that see it at the end.  Its token counts as 2^10, so that R is at least t - 6 there and the weight 2^(t + 6 - R) at most 2^12, whatever is left of the token.  A pair without such values:
 #define PG_APART 0x44800000u                        // 2^10, the bits
-#define PG_ENDLESS 0x71800000u                      // 2^100: weights of up to 2^14 times more would leave fp32, it counts as infinite
+#define PG_ENDLESS 0x71800000u                      // 2^100: up to it the sum of 128 keys of such weights stays in fp32; from it on a value counts as infinite
 __device__ __forceinline__ unsigned int near_or_zero(unsigned int w) {
     return ((w << 16 & 0x7fff0000u) >= PG_APART ? 0u : w & 0xffffu) | ((w & 0x7fff0000u) >= PG_APART ? 0u : w & 0xffff0000u);
 }
@@ -477,7 +477,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                         unsigned int m = max(max(pair_amax(x.x), pair_amax(x.y)), max(pair_amax(x.z), pair_amax(x.w)));
                         if (m >= PG_APART) {
                             x = make_uint4(near_or_zero(x.x), near_or_zero(x.y), near_or_zero(x.z), near_or_zero(x.w));
-                            m = max(max(pair_amax(x.x), pair_amax(x.y)), max(pair_amax(x.z), pair_amax(x.w)));
+                            m = PG_APART;
                             *at = x;
                             const int key = (g0 + t) * PG_BN + row;
                             atomicOr(&s_odd[key >> 5], 1u << (key & 31));
@@ -502,7 +502,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                         unsigned int m = max(max(pair_amax(v[j].x), pair_amax(v[j].y)), max(pair_amax(v[j].z), pair_amax(v[j].w)));
                         if (m >= PG_APART) {
                             v[j] = make_uint4(near_or_zero(v[j].x), near_or_zero(v[j].y), near_or_zero(v[j].z), near_or_zero(v[j].w));
-                            m = max(max(pair_amax(v[j].x), pair_amax(v[j].y)), max(pair_amax(v[j].z), pair_amax(v[j].w)));
+                            m = PG_APART;
                             const int key = (g0 + t) * PG_BN + row;
                             atomicOr(&s_odd[key >> 5], 1u << (key & 31));
                         }
@@ -985,7 +985,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
                     float score = 0.f;
 #pragma unroll 1
                     for (int c = 0; c < HS_HEAD_DIM; ++c) score = fmaf(__bfloat162float(p.q[(size_t)orow * HS_HEAD_DIM + c]), __bfloat162float(p.k_tree[kv + c]), score);
-                    const float weight = ex2_approx(fmaf(score, p.scale_log2, PG_LIFT - mrun));
+                    const float weight = fminf(ex2_approx(fmaf(score, p.scale_log2, PG_LIFT - mrun)), 16384.f);      // (huge scores: this one and the product's may differ by more)
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
                         const float x = __bfloat162float(p.v_tree[kv + ch + c]);

@@ -173,3 +173,25 @@ def test_tokens_of_every_size_weigh_as_they_should(batch, nodes, hq, hkv, tokens
         r = slice(b * nodes, (b + 1) * nodes)
         check(out[r], lse[r], q[r], K, V, k[r], v[r], m)
     ctx.close()
+
+
+@pytest.mark.parametrize("value", [2.0 ** 12, -2.0 ** 62, 2.0 ** 70, 2.0 ** 99])
+@pytest.mark.parametrize("places", ["one", "all", "node"])
+@pytest.mark.parametrize("batch, nodes, hq, hkv, tokens", [(1, 1, 4, 1, 0), (1, 1, 4, 1, 512), (2, 1, 32, 8, 70), (1, 12, 8, 2, 0), (1, 12, 8, 2, 512), (1, 60, 8, 2, 0), (1, 60, 8, 2, 1000),
+                                                            (1, 100, 8, 2, 300), (16, 60, 32, 8, 0)])
+def test_huge_values_among_zeros(batch, nodes, hq, hkv, tokens, places, value):
+    """Trees whose values are zero, or all apart, but for the huge ones."""
+    ctx, pr, cache, K, V, q, k, v = random_case(batch, nodes, hq, hkv, tokens, 41)
+    v.zero_()
+    if places == "all":
+        v[:] = value
+    elif places == "one":
+        v[::nodes, :, 3] = value
+    else:
+        v[::nodes] = value
+    out, lse = run(ctx, pr, cache, q, k, v, [nodes] * batch)
+    assert torch.isfinite(out).all()
+    for b, m in list(enumerate(masks(pr, [nodes] * batch)))[::9]:
+        r = slice(b * nodes, (b + 1) * nodes)
+        check(out[r], lse[r], q[r], K, V, k[r], v[r], m)
+    ctx.close()
