@@ -387,7 +387,9 @@ hs_status hs_kv_append(hs_ctx* ctx, const hs_kv_cache* cache, const void* k, con
 /* The same for the path that hs_accept_path chose: the root and the accepted nodes of sequence b, in order, become tokens
  * kv_len[b] .. kv_len[b] + accept_len[b] of the cache.  k_tree, v_tree: [max_rows][hkv][128] bf16, rows by `layout` as for the
  * attention.  Reads accept_len, path_compact (COMPACT) or path_nodes (ORIGINAL), and both status arrays: a sequence with a
- * status other than 0 appends nothing.  Of a path longer than path_cap the first path_cap tokens are appended, with HS_ERR_BAD_PAGE. */
+ * status other than 0 appends nothing.  Of a path longer than path_cap the first path_cap tokens are appended, with HS_ERR_BAD_PAGE.  An entry that
+ * is no node of its tree (COMPACT: no kept one), or whose row lies outside [0, max_rows), leaves its token's slot unwritten, with HS_ERR_BAD_PAGE too:
+ * len_out counts the path as hs_accept_path gave it either way, so read the error word ahead of lengths that such a path may have reached. */
 hs_status hs_kv_append_path(hs_ctx* ctx, const hs_kv_cache* cache, const hs_pruned_tree* pruned,
                             const hs_accept_out* accept, int32_t layout, const int32_t* node_off, const void* k_tree,
                             const void* v_tree, int32_t max_rows, int32_t* len_out, hs_stream stream);

@@ -218,12 +218,15 @@ kv_append_path_kernel(const KvPages c, const AppendPath a, const __nv_bfloat16* 
     long long at = -1;
     if (b < (unsigned int)c.batch) {
         // one round trip for what says whether and where there is a row
-        const int n = tokens(b), node = a.path[(size_t)b * a.path_cap + i], base = a.row_base[b], keep = a.n_keep[b];
+        const int n = tokens(b), node = a.path[(size_t)b * a.path_cap + i], base = a.row_base[b], nodes = a.compact ? a.n_keep[b] : a.row_base[b + 1] - base;
         const long long row = (long long)base + node, pos = (long long)kv_length(c, b) + i;
-        if (i < n && node >= 0 && !(a.compact && node >= keep) && row >= 0 && row < a.max_rows) {      // (else not a path of this tree)
+        const bool there = node >= 0 && node < nodes && row >= 0 && row < a.max_rows;
+        if (i < n && there) {
             x.load((is_v ? v : k) + (row * c.hkv + head) * HS_HEAD_DIM, sub);
             if (pos < ((long long)c.max_pages << c.log_page)) at = kv_row(c, b, (int)pos);
             else kv_bad_page(c.err);
+        } else if (i < n) {
+            kv_bad_page(c.err);                                    // not a path of this tree, or of these rows: its token stays unwritten
         }
     }
     if (at < 0) x.w[0] = x.w[1] = make_uint4(0u, 0u, 0u, 0u);

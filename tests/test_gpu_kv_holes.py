@@ -1,0 +1,75 @@
+"""Appends whose rows are not all there: each alone in a context of its own, so that its own error is the one that is read."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+from paged_util import i32
+from paper_2505_13254_b200 import binding as hb
+
+pytestmark = pytest.mark.gpu
+
+
+def pool(batch, hkv=2, page=16):
+    cache = hb.KvCache.empty(batch * 2, hkv, page, i32(np.arange(batch * 2).reshape(batch, 2).tolist()))
+    for t in (cache.k, cache.v, cache.k_scale, cache.v_scale):
+        t.fill_(77)
+    return cache
+
+
+def rows(n, hkv=2, seed=0):
+    return torch.randn(n, hkv, 128, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)).bfloat16()
+
+
+def bundles(paths, keep, total):
+    batch, cap = len(paths), 8
+    pr, acc = hb.PrunedTree(total, batch, "cuda"), hb.AcceptOut(batch, cap, "cuda")
+    pr.n_keep.copy_(i32(keep))
+    pr.keep_off.copy_(i32(np.concatenate([[0], np.cumsum(keep)]).tolist()))
+    pr.status.zero_()
+    acc.status.zero_()
+    acc.accept_len.copy_(i32([len(p) - 1 for p in paths]))
+    table = np.full((batch, cap), -1)
+    for b, p in enumerate(paths):
+        table[b, :len(p)] = p
+    for t in (acc.path_compact, acc.path_nodes):
+        t.copy_(torch.from_numpy(table).int())
+    return pr, acc
+
+
+@pytest.mark.parametrize("layout, path, keep, max_rows", [
+    (hb.HS_ROWS_COMPACT, [0, -1, 2], 5, 10),                             # no node
+    (hb.HS_ROWS_COMPACT, [0, 5, 2], 5, 10),                              # behind the kept nodes
+    (hb.HS_ROWS_COMPACT, [0, 1, 2], 5, 7),                               # a row behind the arrays (sequence 1 starts at row 5)
+    (hb.HS_ROWS_ORIGINAL, [0, -3, 2], 5, 10), (hb.HS_ROWS_ORIGINAL, [0, 9, 2], 5, 10), (hb.HS_ROWS_ORIGINAL, [0, 5, 2], 5, 12),
+    (hb.HS_ROWS_COMPACT, [0, 1, (1 << 31) - 1], 5, 10), (hb.HS_ROWS_ORIGINAL, [0, 1, (1 << 31) - 1], 5, 10),
+])
+def test_an_entry_of_a_path_without_a_row_is_an_error(layout, path, keep, max_rows):
+    ctx, cache = hb.Context(0, 1 << 20), pool(2)
+    pr, acc = bundles([[0, 1], path], [5, keep], 10)
+    k, node_off, length = rows(max_rows), i32([0, 5, 10]), torch.zeros(2, dtype=torch.int32, device="cuda")
+    hb.hs_kv_append_path(ctx, cache, pr, acc, k, k, layout=layout, node_off=node_off if layout == hb.HS_ROWS_ORIGINAL else None, len_out=length)
+    assert hb.hs_device_error(ctx) == hb.HS_ERR_BAD_PAGE
+    want = [t.cpu().numpy() for t in pool(2).__dict__.values() if torch.is_tensor(t)][:4]
+    table, x = cache.page_table.tolist(), k.double().cpu().numpy()
+    for b, p in enumerate(([0, 1], path)):
+        for i, node in enumerate(p):
+            if 0 <= node < keep and 5 * b + node < max_rows:
+                for data, scale in ((want[0], want[2]), (want[1], want[3])):
+                    paged.append(data, scale, table, 16, b, i, x[5 * b + node][None])
+    for got, w in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), want):
+        assert np.array_equal(got.cpu().numpy(), w)
+    assert length.tolist() == [2, 3]
+    ctx.close()
+    # without the entry: no error
+    ctx = hb.Context(0, 1 << 20)
+    pr, acc = bundles([[0, 1], [0, 1, 2]], [5, 5], 10)
+    hb.hs_kv_append_path(ctx, pool(2), pr, acc, rows(10), rows(10), layout=layout, node_off=node_off if layout == hb.HS_ROWS_ORIGINAL else None)
+    assert hb.hs_device_error(ctx) == 0
+    # and a sequence that was skipped has no path to look at
+    acc.path_compact.fill_(-9)
+    acc.path_nodes.fill_(-9)
+    acc.status.fill_(3)
+    hb.hs_kv_append_path(ctx, pool(2), pr, acc, rows(10), rows(10), layout=layout, node_off=node_off if layout == hb.HS_ROWS_ORIGINAL else None)
+    assert hb.hs_device_error(ctx) == 0
+    ctx.close()
