@@ -376,9 +376,9 @@ typedef struct {
 
 /* Quantises and writes rows row_off[b] .. row_off[b+1]-1 of k and v as tokens kv_len[b], kv_len[b]+1, .. of sequence b.
  * Row r, head h, value i lies at k[r * token_stride + h * head_stride + i] (strides in elements, multiples of 8 for bf16, 4
- * for f32; bases 16-byte aligned): a slice of a fused projection's output will do.  n_rows (host): rows of the arrays, at least row_off[batch];
- * rows from row_off[batch] on are left out.  kv_len itself is not advanced (all layers of a step append at the same one):
- * len_out (nullable, another array than kv_len) receives kv_len[b] + the rows of b.  Tokens behind max_pages * page_size
+ * for f32; bases 16-byte aligned): a slice of a fused projection's output will do.  n_rows (host): rows of the arrays; those from
+ * row_off[batch] on are left out, and where row_off[batch] is larger the rows that are missing are, with HS_ERR_SHAPE in the error word;
+ * len_out does not count them.  kv_len itself is not advanced (all layers of a step append at the same one): len_out (nullable, another array than kv_len) receives kv_len[b] + the rows of b.  Tokens behind max_pages * page_size
  * are dropped with HS_ERR_BAD_PAGE, and len_out stops there. */
 hs_status hs_kv_append(hs_ctx* ctx, const hs_kv_cache* cache, const void* k, const void* v, hs_dtype dtype,
                        int64_t token_stride, int64_t head_stride, const int32_t* row_off, int32_t n_rows,

@@ -161,7 +161,9 @@ kv_append_kernel(const KvPages c, const AppendRows a, const T* __restrict__ k, c
                  const long long head_stride, int* len_out) {
     pdl_launch_dependents();
     pdl_wait();
-    if (write_lengths(c, len_out, [&](int b) { return a.row_off[b + 1] - a.row_off[b]; })) return;
+    // (rows that the offsets name behind the arrays are none)
+    if (blockIdx.x == 0 && threadIdx.x == 0 && (a.row_off[c.batch] > a.n_rows || a.row_off[0] < 0)) atomicCAS(c.err, 0, (int)HS_ERR_SHAPE);
+    if (write_lengths(c, len_out, [&](int b) { return min(a.row_off[b + 1], a.n_rows) - min(a.row_off[b], a.n_rows); })) return;
     const int lane = threadIdx.x & 31, sub = lane & 7;
     const bool is_v = lane & 8;
     const unsigned int first = (blockIdx.x * (KV_THREADS / 32) + (threadIdx.x >> 5)) * (2 * KV_STEPS), total = (unsigned int)a.n_rows * (unsigned int)c.hkv;
@@ -294,9 +296,9 @@ hs_status hs_launch_kv_append(hs_ctx* ctx, const hs_kv_cache* cache, const void*
     const KvPages c = kv_pages(cache, ctx->counters + HS_CNT_ERROR);
     const AppendRows a{row_off, n_rows};
     const long long items = (long long)n_rows * cache->hkv;
-    if (items == 0 && !len_out) return HS_OK;
     if (items > 0x7fffffffll) return HS_ERR_SHAPE;
-    const dim3 grid(blocks_of(items, KV_STEPS, len_out != nullptr)), block(KV_THREADS), one(1, 1, 1);
+    // (without rows the offsets are looked at all the same)
+    const dim3 grid(max(blocks_of(items, KV_STEPS, len_out != nullptr), 1u)), block(KV_THREADS), one(1, 1, 1);
     const long long ts = token_stride, hs = head_stride;
     cudaError_t e;
     if (dtype == HS_BF16)

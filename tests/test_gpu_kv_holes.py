@@ -73,3 +73,34 @@ def test_an_entry_of_a_path_without_a_row_is_an_error(layout, path, keep, max_ro
     hb.hs_kv_append_path(ctx, pool(2), pr, acc, rows(10), rows(10), layout=layout, node_off=node_off if layout == hb.HS_ROWS_ORIGINAL else None)
     assert hb.hs_device_error(ctx) == 0
     ctx.close()
+
+
+@pytest.mark.parametrize("with_length", [True, False])
+@pytest.mark.parametrize("n_rows, off, lengths", [
+    (6, [0, 4, 9], [4, 2]), (4, [0, 4, 9], [4, 0]), (3, [0, 4, 9], [3, 0]), (0, [0, 4, 9], [0, 0]), (6, [2, 4, 9], [2, 2]), (3, [5, 7, 9], [0, 0]),
+])
+def test_rows_that_the_offsets_name_behind_the_arrays_are_an_error(n_rows, off, lengths, with_length):
+    ctx, cache = hb.Context(0, 1 << 20), pool(2)
+    x, length = rows(max(n_rows, 1))[:n_rows], torch.full((2,), -1, dtype=torch.int32, device="cuda")
+    hb.hs_kv_append(ctx, cache, x, x, i32(off), len_out=length if with_length else None)
+    assert hb.hs_device_error(ctx) == hb.HS_ERR_SHAPE
+    want = [t.cpu().numpy() for t in pool(2).__dict__.values() if torch.is_tensor(t)][:4]
+    table, host = cache.page_table.tolist(), x.double().cpu().numpy()
+    for b in range(2):
+        part = host[min(off[b], n_rows):min(off[b + 1], n_rows)]
+        assert len(part) == lengths[b]
+        for data, scale in ((want[0], want[2]), (want[1], want[3])):
+            paged.append(data, scale, table, 16, b, 0, part)
+    for got, w in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), want):
+        assert np.array_equal(got.cpu().numpy(), w)
+    assert length.tolist() == (lengths if with_length else [-1, -1])
+    ctx.close()
+
+
+def test_rows_of_the_arrays_behind_the_offsets_are_none():
+    ctx, cache = hb.Context(0, 1 << 20), pool(2)
+    length = torch.zeros(2, dtype=torch.int32, device="cuda")
+    hb.hs_kv_append(ctx, cache, rows(12), rows(12), i32([0, 4, 9]), len_out=length)
+    hb.hs_kv_append(ctx, cache, rows(9), rows(9), i32([0, 4, 9]))
+    assert hb.hs_device_error(ctx) == 0 and length.tolist() == [4, 5]
+    ctx.close()
