@@ -521,6 +521,8 @@ def make_rope(head_dim: int = 128, rotary_dim: Optional[int] = None, *, base: fl
     rotary_dim = head_dim if rotary_dim is None else rotary_dim
     freq = None
     if inv_freq is not None:
+        if scaling != "table":
+            raise ValueError("inv_freq is read with scaling=\"table\" only")
         freq = [float(f) for f in inv_freq]
         if len(freq) != rotary_dim // 2:
             raise ValueError("inv_freq has rotary_dim / 2 frequencies")

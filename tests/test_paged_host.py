@@ -208,3 +208,9 @@ def test_lanes_that_waited_alone_meet_again_ahead_of_tensor_memory():
 def test_pages_are_checked_before_they_are_used():
     assert re.search(r"if \(\(unsigned int\)page >= \(unsigned int\)c\.n_pages\) \{\s*kv_bad_page\(c\.err\);\s*return -1;", text("kv_page.cuh"))
     assert re.search(r"if \(\(unsigned int\)id >= \(unsigned int\)p\.c\.n_pages\) \{.*?kv_bad_page\(err\);\s*id = 0;", text("tree_attn_paged.cu"), re.S)
+
+
+@pytest.mark.parametrize("scaling", ["none", "linear", "ntk", "llama3", "yarn"])
+def test_frequencies_that_would_not_be_read_are_a_python_error(scaling):
+    with pytest.raises(ValueError):
+        hb.make_rope(32, scaling=scaling, factor=4.0, original_len=4096, inv_freq=[0.25] * 16)
