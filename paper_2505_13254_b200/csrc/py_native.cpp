@@ -10,7 +10,7 @@
 
 namespace {
 
-PyObject *n_data_ptr, *n_stride, *n_size, *n_dtype, *o_zero, *o_one, *o_two, *t_f32, *t_bf16, *t_i32;
+PyObject *n_data_ptr, *n_contiguous, *n_stride, *n_size, *n_dtype, *o_zero, *o_one, *o_two, *t_f32, *t_bf16, *t_i32;
 
 struct Name {
     const char* text;
@@ -128,6 +128,15 @@ struct Reader {
         else for (int i = 0; i < 3; ++i) out[i] = integer(PyTuple_GET_ITEM(r, i));
         Py_DECREF(r);
     }
+    // (the calls take the entries of a list, of a table of sums, to lie side by side)
+    void contiguous(PyObject* t) {
+        if (bad) return;
+        PyObject* args[] = {nullptr, t};
+        PyObject* r = PyObject_VectorcallMethod(n_contiguous, args + 1, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
+        if (!r) { bad = true; return; }
+        if (r != Py_True) fail("a contiguous tensor is expected");
+        Py_DECREF(r);
+    }
     // a tensor of `count` entries, or None
     void* list(PyObject* t, long long count, const char* why, PyObject* type = t_i32) {
         if (bad || t == Py_None) return nullptr;
@@ -140,6 +149,7 @@ struct Reader {
             PyErr_Format(PyExc_TypeError, "a tensor of %S is expected, got %S", type, d);
             return nullptr;
         }
+        contiguous(t);
         return ptr(t);
     }
     // a bundle's `status` has an entry for each of `batch` sequences
@@ -535,13 +545,14 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nu
 
 PyMODINIT_FUNC PyInit__native(void) {
     n_data_ptr = PyUnicode_InternFromString("data_ptr");
+    n_contiguous = PyUnicode_InternFromString("is_contiguous");
     n_stride = PyUnicode_InternFromString("stride");
     n_size = PyUnicode_InternFromString("size");
     n_dtype = PyUnicode_InternFromString("dtype");
     o_zero = PyLong_FromLong(0);
     o_one = PyLong_FromLong(1);
     o_two = PyLong_FromLong(2);
-    if (!n_data_ptr || !n_stride || !n_size || !n_dtype || !o_zero || !o_one || !o_two ||
+    if (!n_data_ptr || !n_contiguous || !n_stride || !n_size || !n_dtype || !o_zero || !o_one || !o_two ||
         !intern_all(k_tree, 5) || !intern_all(k_quant, 14) || !intern_all(k_pruned, 11) || !intern_all(k_accept, 9) ||
         !intern_all(k_expand, 12) || !intern_all(k_policy, 9) || !intern_all(k_cache, 12) || !intern_all(k_rope, 1))
         return nullptr;

@@ -214,3 +214,39 @@ def test_pages_are_checked_before_they_are_used():
 def test_frequencies_that_would_not_be_read_are_a_python_error(scaling):
     with pytest.raises(ValueError):
         hb.make_rope(32, scaling=scaling, factor=4.0, original_len=4096, inv_freq=[0.25] * 16)
+
+
+def spread(t):
+    """The same entries, not side by side."""
+    wide = torch.zeros(*t.shape, 2, dtype=t.dtype)
+    wide[..., 0] = t
+    return wide[..., 0]
+
+
+@pytest.mark.parametrize("call", [
+    lambda n, c, pr, acc, o: n.kv_append(0, c, rows(), rows(), spread(o), None, 0),
+    lambda n, c, pr, acc, o: n.kv_append(0, c, rows(), rows(), o, spread(c.kv_len), 0),
+    lambda n, c, pr, acc, o: n.kv_append(0, c, rows(), rows(), o[:1].expand(3), None, 0),                  # one entry, not three
+    lambda n, c, pr, acc, o: n.kv_append_path(0, c, pr, acc, 1, spread(o), rows(), rows(), None, 0),
+    lambda n, c, pr, acc, o: n.kv_append_path(0, c, pr, acc, 0, None, rows(), rows(), spread(c.kv_len), 0),
+    lambda n, c, pr, acc, o: n.kv_read(0, c, spread(o), None, rows(), rows(), 0),
+    lambda n, c, pr, acc, o: n.kv_read(0, c, o, spread(c.kv_len), rows(), rows(), 0),
+    lambda n, c, pr, acc, o: n.tree_verify_attention_paged(0, pr, c, rows(), rows(), rows(), 4, 9, 1, spread(o), None, rows(), None, 0),
+    lambda n, c, pr, acc, o: n.tree_verify_attention_paged(0, pr, c, rows(), rows(), rows(), 4, 9, 0, None, None, rows(), torch.zeros(2, 4).t(), 0),
+    lambda n, c, pr, acc, o: n.tree_verify_attention_paged(0, pr, c, rows(), rows(), rows(), 4, 9, 0, None, None, rows(), torch.zeros(1).expand(4, 2), 0),
+    lambda n, c, pr, acc, o: n.rotary(0, hb.make_rope(128), spread(o), rows(3), rows(3), None, None, 0),
+    lambda n, c, pr, acc, o: n.rotary(0, hb.make_rope(128), o[:1].expand(3), rows(3), rows(3), None, None, 0),
+    lambda n, c, pr, acc, o: n.rotary_tree(0, hb.make_rope(128), pr, spread(c.kv_len), 4, 0, None, rows(), rows(), None, None, 0),
+    lambda n, c, pr, acc, o: n.rotary_tree(0, hb.make_rope(128), pr, c.kv_len, 4, 1, spread(o), rows(), rows(), None, None, 0),
+])
+def test_lists_whose_entries_do_not_lie_side_by_side_are_python_errors(call):
+    with pytest.raises(ValueError):
+        call(hb.native(), cache(), hb.PrunedTree(4, 2, "cpu"), hb.AcceptOut(2, 4, "cpu"), torch.zeros(3, dtype=torch.int32))
+
+
+def test_lists_of_one_entry_have_no_stride():
+    c, off = cache(batch=1), torch.zeros(2, dtype=torch.int32)
+    one = torch.zeros(4, 3, dtype=torch.int32)[:1, 1]
+    assert one.stride() == (3,)
+    assert hb.native().kv_append(0, c, rows(), rows(), off, one, 0) == hb.HS_ERR_INVALID_ARG
+    assert hb.native().rotary(0, hb.make_rope(128), one, rows(1), rows(1), None, None, 0) == hb.HS_ERR_INVALID_ARG
