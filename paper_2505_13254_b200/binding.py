@@ -449,6 +449,7 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale, self.page_table, self.kv_len = k, v, k_scale, v_scale, page_table, kv_len
         self.n_pages, self.hkv, self.page_size, self.head_dim = k.shape
         self.batch, self.max_pages = page_table.shape
+        self.device_index = k.get_device()
 
     def __setattr__(self, name, value):
         old = self.__dict__.get(name)

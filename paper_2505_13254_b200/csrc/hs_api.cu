@@ -275,6 +275,9 @@ extern "C" hs_status hs_philox_uniforms(hs_ctx* ctx, uint64_t seed, uint64_t off
     return hs_launch_philox(seed, offset, b, node, stream_id, count, out, (cudaStream_t)stream);
 }
 
+// for the Python binding's native module
+extern "C" int hs_context_device(const hs_ctx* ctx) { return ctx->device; }
+
 // ---- the paged cache ---------------------------------------------------------------------------------------------------
 static hs_status cache_check(const hs_kv_cache* c) {
     if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->page_table || !c->kv_len) return HS_ERR_INVALID_ARG;

@@ -8,9 +8,11 @@
 
 #include "../../include/heterospec.h"
 
+extern "C" int hs_context_device(const hs_ctx* ctx);        // (of the library, not of its interface)
+
 namespace {
 
-PyObject *n_data_ptr, *n_contiguous, *n_stride, *n_size, *n_dtype, *o_zero, *o_one, *o_two, *t_f32, *t_bf16, *t_i32;
+PyObject *n_data_ptr, *n_contiguous, *n_get_device, *n_numel, *n_stride, *n_size, *n_dtype, *o_zero, *o_one, *o_two, *t_f32, *t_bf16, *t_i32;
 
 struct Name {
     const char* text;
@@ -28,7 +30,7 @@ Name k_expand[] = {{"batch"}, {"cap"}, {"top_k"}, {"n_cand"}, {"parent"}, {"toke
 Name k_policy[] = {{"thresholds"}, {"d_base"}, {"alpha"}, {"n_default"}, {"top_k"}, {"gamma_pct"}, {"phi_mode"},
                    {"pstar_mode"}, {"entropy_mode"}};
 Name k_cache[] = {{"batch"}, {"hkv"}, {"head_dim"}, {"page_size"}, {"n_pages"}, {"max_pages"}, {"k"}, {"v"}, {"k_scale"},
-                  {"v_scale"}, {"page_table"}, {"kv_len"}};
+                  {"v_scale"}, {"page_table"}, {"kv_len"}, {"device_index"}};
 Name k_rope[] = {{"address"}};
 
 // fields of k_pruned and k_accept, as bits
@@ -47,6 +49,7 @@ bool intern_all(Name* k, size_t n) {
 // Reads arguments and fields; after a failed read `bad` stays set, the Python error with it, and reads return 0.
 struct Reader {
     bool bad = false;
+    long long device = -2;          // of the tensors that were asked for theirs: -2 none yet, -1 host memory, -3 several
 
     long long integer(PyObject* o) {
         if (bad) return 0;
@@ -128,19 +131,41 @@ struct Reader {
         else for (int i = 0; i < 3; ++i) out[i] = integer(PyTuple_GET_ITEM(r, i));
         Py_DECREF(r);
     }
-    // (the calls take the entries of a list, of a table of sums, to lie side by side)
-    void contiguous(PyObject* t) {
+    void met(long long d) { device = device == -2 || device == d ? d : -3; }
+    void locate(PyObject* t) {
         if (bad) return;
         PyObject* args[] = {nullptr, t};
-        PyObject* r = PyObject_VectorcallMethod(n_contiguous, args + 1, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
+        PyObject* r = PyObject_VectorcallMethod(n_get_device, args + 1, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
         if (!r) { bad = true; return; }
-        if (r != Py_True) fail("a contiguous tensor is expected");
+        met(integer(r));
         Py_DECREF(r);
+    }
+    // (a pointer into host memory, or another device's, would fault the context's)
+    void here(const hs_ctx* ctx) {
+        if (!bad && ctx && device != hs_context_device(ctx)) fail("the tensors of a call are on the context's device");
+    }
+    bool contiguous(PyObject* t) {
+        if (bad) return false;
+        PyObject* args[] = {nullptr, t};
+        PyObject* r = PyObject_VectorcallMethod(n_contiguous, args + 1, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
+        if (!r) { bad = true; return false; }
+        Py_DECREF(r);
+        return r == Py_True;
+    }
+    // entries of a tensor (a third of what size(0) costs)
+    long long numel(PyObject* t) {
+        if (bad) return 0;
+        PyObject* args[] = {nullptr, t};
+        PyObject* r = PyObject_VectorcallMethod(n_numel, args + 1, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
+        if (!r) { bad = true; return 0; }
+        const long long v = integer(r);
+        Py_DECREF(r);
+        return v;
     }
     // a tensor of `count` entries, or None
     void* list(PyObject* t, long long count, const char* why, PyObject* type = t_i32) {
         if (bad || t == Py_None) return nullptr;
-        if (size(t, o_zero) != count && !bad) return fail(why);
+        if (numel(t) != count && !bad) return fail(why);
         PyObject* d = bad ? nullptr : PyObject_GetAttr(t, n_dtype);
         if (!d) { bad = true; return nullptr; }
         Py_DECREF(d);
@@ -149,7 +174,8 @@ struct Reader {
             PyErr_Format(PyExc_TypeError, "a tensor of %S is expected, got %S", type, d);
             return nullptr;
         }
-        contiguous(t);
+        if (!contiguous(t) && !bad) return fail("a contiguous tensor is expected");      // (the calls take the entries to lie side by side)
+        locate(t);
         return ptr(t);
     }
     // a bundle's `status` has an entry for each of `batch` sequences
@@ -157,7 +183,7 @@ struct Reader {
         if (bad) return;
         PyObject* v = PyObject_GetAttr(o, status.str);
         if (!v) { bad = true; return; }
-        if (size(v, o_zero) != batch && !bad) fail(why);
+        if (numel(v) != batch && !bad) fail(why);
         Py_DECREF(v);
     }
     void tree(PyObject* o, hs_tree_batch* t) {
@@ -177,6 +203,7 @@ struct Reader {
         int32_t* ints = &c->batch;
         for (int i = 0; i < 6; ++i) ints[i] = field_int(o, k_cache[i]);
         pointers(o, k_cache + 6, 6, &c->k);
+        met(field_int(o, k_cache[12]));
     }
     const hs_rope* rope(PyObject* o) {
         if (bad) return nullptr;
@@ -192,18 +219,24 @@ struct Reader {
         if (bad) return nullptr;
         const hs_dtype dt = dtype(t, "heads");
         if (bad) return nullptr;
-        long long sizes[3] = {0, 0, 0}, strides[3] = {0, 0, 0};
+        long long sizes[3] = {0, 0, 0}, strides[3] = {0, 0, 1};
         three(n_size, t, sizes);
-        three(n_stride, t, strides);
         if (bad) return nullptr;
         *rows = sizes[0]; *n_heads = sizes[1]; *dim = sizes[2];
+        if (contiguous(t)) {
+            strides[0] = sizes[1] * sizes[2];
+            strides[1] = sizes[2];
+        } else {
+            three(n_stride, t, strides);
+            if (whole && !bad) return fail("a contiguous tensor [rows, heads, values] is expected");
+        }
+        if (bad) return nullptr;
         *token_stride = strides[0]; *head_stride = strides[1];
         if (dt != want) return fail("tensors of one call have one type");
         if (*rows > 0 && strides[2] != 1) return fail("the values of a head lie side by side");
-        if (whole && *rows > 0 && (*token_stride != *n_heads * *dim || (*n_heads > 1 && *head_stride != *dim)))
-            return fail("a contiguous tensor [rows, heads, values] is expected");
         if (*n_heads == 1) *head_stride = *dim;              // (of a single head the stride means nothing)
         if (*rows <= 1 && *token_stride < *n_heads * *dim) *token_stride = *n_heads * *dim;
+        locate(t);
         return ptr(t);
     }
     void* fail(const char* why) {
@@ -266,6 +299,13 @@ bool arity(Py_ssize_t got, Py_ssize_t want) {
         st = call;                                      \
         Py_END_ALLOW_THREADS                            \
         return PyLong_FromLong((long)st);               \
+    } while (0)
+
+// the same for calls whose tensors were asked for their device
+#define HS_DONE_HERE(call)                              \
+    do {                                                \
+        r.here(r.ctx(a[0]));                            \
+        HS_DONE(call);                                  \
     } while (0)
 
 // (ctx, tree, logits, policy, quant, stream)
@@ -404,7 +444,7 @@ HS_NATIVE(kv_append) {
     if (!r.bad && (heads != c.hkv || dim != c.head_dim || rows > 0x7fffffffll)) r.fail("k and v are [rows, hkv, head_dim] of the cache");
     const int32_t* off = (const int32_t*)r.list(a[4], c.batch + 1ll, k_offsets);
     int32_t* len = (int32_t*)r.list(a[5], c.batch, k_entries);
-    HS_DONE(hs_kv_append(ctx, &c, k, v, dt, ts, hs, off, (int)rows, len, stream));
+    HS_DONE_HERE(hs_kv_append(ctx, &c, k, v, dt, ts, hs, off, (int)rows, len, stream));
 }
 // (ctx, cache, pruned, accept, layout, node_off | None, k_tree, v_tree, len_out | None, stream)
 HS_NATIVE(kv_append_path) {
@@ -426,7 +466,7 @@ HS_NATIVE(kv_append_path) {
     const void* v = r.heads(a[7], true, HS_BF16, &rows2, &heads2, &dim2, &ts, &hs);
     if (!r.bad && (rows != rows2 || heads != heads2 || dim != dim2 || heads != c.hkv || dim != c.head_dim)) r.fail("k_tree and v_tree are [rows, hkv, head_dim] of the cache");
     int32_t* len = (int32_t*)r.list(a[8], c.batch, k_entries);
-    HS_DONE(hs_kv_append_path(ctx, &c, &t, &o, layout, node_off, k, v, (int)rows, len, stream));
+    HS_DONE_HERE(hs_kv_append_path(ctx, &c, &t, &o, layout, node_off, k, v, (int)rows, len, stream));
 }
 // (ctx, cache, row_off, first | None, k_out, v_out, stream)
 HS_NATIVE(kv_read) {
@@ -442,7 +482,7 @@ HS_NATIVE(kv_read) {
     void* v = r.heads(a[5], false, dt, &rows2, &heads2, &dim2, &ts2, &hs2);
     if (!r.bad && (rows != rows2 || heads != heads2 || dim != dim2 || ts != ts2 || hs != hs2)) r.fail("k_out and v_out have one shape and one stride");
     if (!r.bad && (heads != c.hkv || dim != c.head_dim || rows > 0x7fffffffll)) r.fail("k_out and v_out are [rows, hkv, head_dim] of the cache");
-    HS_DONE(hs_kv_read(ctx, &c, off, first, (int)rows, k, v, dt, ts, hs, stream));
+    HS_DONE_HERE(hs_kv_read(ctx, &c, off, first, (int)rows, k, v, dt, ts, hs, stream));
 }
 // (ctx, pruned, cache, q, k_tree, v_tree, max_nodes, max_kv_len, layout, node_off | None, sm_scale | None, out, lse | None, stream)
 HS_NATIVE(tree_verify_attention_paged) {
@@ -467,9 +507,9 @@ HS_NATIVE(tree_verify_attention_paged) {
     d.layout = (int)r.integer(a[8]);
     d.node_off = (const int32_t*)r.list(a[9], c.batch + 1ll, k_offsets);
     d.sm_scale = a[10] == Py_None ? 0.08838834764831845f : (float)r.real(a[10]);      // 1 / sqrt(128)
-    float* lse = (float*)r.list(a[12], rows[0], "lse_out is [rows, hq]", t_f32);
+    float* lse = (float*)r.list(a[12], rows[0] * heads[0], "lse_out is [rows, hq]", t_f32);
     if (lse && r.size(a[12], o_one) != heads[0] && !r.bad) r.fail("lse_out is [rows, hq]");
-    HS_DONE(hs_tree_verify_attention_paged(ctx, &t, &c, &d, x[0], x[1], x[2], x[3], lse, stream));
+    HS_DONE_HERE(hs_tree_verify_attention_paged(ctx, &t, &c, &d, x[0], x[1], x[2], x[3], lse, stream));
 }
 // q or k with its output, as hs_heads
 void head_pair(Reader& r, PyObject* in, PyObject* out, hs_dtype dt, hs_heads* x, long long* rows, long long* dim) {
@@ -496,7 +536,7 @@ HS_NATIVE(rotary) {
     const int32_t* pos = (const int32_t*)r.list(a[2], rows, "one position for each row");
     if (!r.bad && rows > 0x7fffffffll) r.fail("one position for each row");
     if (!r.bad && dim != rope->head_dim) r.fail("the head size is not the one of the frequencies");
-    HS_DONE(hs_rotary(ctx, rope, pos, (int)rows, &q, with_k ? &k : nullptr, dt, stream));
+    HS_DONE_HERE(hs_rotary(ctx, rope, pos, (int)rows, &q, with_k ? &k : nullptr, dt, stream));
 }
 // (ctx, rope, pruned, kv_len, max_nodes, layout, node_off | None, q, q_out, k | None, k_out | None, stream)
 HS_NATIVE(rotary_tree) {
@@ -505,7 +545,7 @@ HS_NATIVE(rotary_tree) {
     const hs_rope* rope = r.rope(a[1]);
     hs_pruned_tree t;
     r.some(a[2], k_pruned, 11, PRUNED_N_KEEP | PRUNED_KEEP_OFF | PRUNED_KEEP_IDX | PRUNED_NEW_DEPTH | PRUNED_STATUS, &t);
-    const long long batch = r.size(a[3], o_zero);
+    const long long batch = r.numel(a[3]);
     const int32_t* kv_len = (const int32_t*)r.list(a[3], batch, k_entries);
     r.batch_of(a[2], k_pruned[10], batch, k_batch);
     const int max_nodes = (int)r.integer(a[4]), layout = (int)r.integer(a[5]);
@@ -520,7 +560,7 @@ HS_NATIVE(rotary_tree) {
         if (!r.bad && (rows2 != rows || dim2 != dim)) r.fail("k has the rows and the head size of q");
     }
     if (!r.bad && dim != rope->head_dim) r.fail("the head size is not the one of the frequencies");
-    HS_DONE(hs_rotary_tree(ctx, rope, &t, kv_len, (int)batch, max_nodes, (int)rows, layout, node_off, &q, with_k ? &k : nullptr, dt, stream));
+    HS_DONE_HERE(hs_rotary_tree(ctx, rope, &t, kv_len, (int)batch, max_nodes, (int)rows, layout, node_off, &q, with_k ? &k : nullptr, dt, stream));
 }
 
 // setup(torch.float32, torch.bfloat16, torch.int32)
@@ -546,15 +586,17 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nu
 PyMODINIT_FUNC PyInit__native(void) {
     n_data_ptr = PyUnicode_InternFromString("data_ptr");
     n_contiguous = PyUnicode_InternFromString("is_contiguous");
+    n_get_device = PyUnicode_InternFromString("get_device");
+    n_numel = PyUnicode_InternFromString("numel");
     n_stride = PyUnicode_InternFromString("stride");
     n_size = PyUnicode_InternFromString("size");
     n_dtype = PyUnicode_InternFromString("dtype");
     o_zero = PyLong_FromLong(0);
     o_one = PyLong_FromLong(1);
     o_two = PyLong_FromLong(2);
-    if (!n_data_ptr || !n_contiguous || !n_stride || !n_size || !n_dtype || !o_zero || !o_one || !o_two ||
+    if (!n_data_ptr || !n_contiguous || !n_get_device || !n_numel || !n_stride || !n_size || !n_dtype || !o_zero || !o_one || !o_two ||
         !intern_all(k_tree, 5) || !intern_all(k_quant, 14) || !intern_all(k_pruned, 11) || !intern_all(k_accept, 9) ||
-        !intern_all(k_expand, 12) || !intern_all(k_policy, 9) || !intern_all(k_cache, 12) || !intern_all(k_rope, 1))
+        !intern_all(k_expand, 12) || !intern_all(k_policy, 9) || !intern_all(k_cache, 13) || !intern_all(k_rope, 1))
         return nullptr;
     return PyModule_Create(&module);
 }

@@ -104,3 +104,24 @@ def test_rows_of_the_arrays_behind_the_offsets_are_none():
     hb.hs_kv_append(ctx, cache, rows(9), rows(9), i32([0, 4, 9]))
     assert hb.hs_device_error(ctx) == 0 and length.tolist() == [4, 5]
     ctx.close()
+
+
+def test_one_tensor_in_host_memory_is_refused():
+    ctx, cache, rope = hb.Context(0, 1 << 20), pool(1), hb.make_rope(128)
+    pr, acc = bundles([[0, 1]], [4], 4)
+    k, q, off, length = rows(4), rows(4, 8), i32([0, 4]), i32([0])
+    host = hb.KvCache(*(t.cpu() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.page_table, cache.kv_len)))
+    tree = dict(max_nodes=4, max_kv_len=9)
+    for call in (lambda: hb.hs_kv_append(ctx, cache, k.cpu(), k, off), lambda: hb.hs_kv_append(ctx, cache, k, k.cpu(), off),
+                 lambda: hb.hs_kv_append(ctx, cache, k, k, off.cpu()), lambda: hb.hs_kv_append(ctx, cache, k, k, off, len_out=length.cpu()),
+                 lambda: hb.hs_kv_append(ctx, host, k, k, off), lambda: hb.hs_kv_append_path(ctx, cache, pr, acc, k, k.cpu()),
+                 lambda: hb.hs_kv_append_path(ctx, host, pr, acc, k, k), lambda: hb.hs_kv_read(ctx, cache, off, k_out=k, v_out=k.cpu()),
+                 lambda: hb.hs_kv_read(ctx, cache, off, k_out=k, v_out=k, first=length.cpu()), lambda: hb.hs_rotary(ctx, rope, i32([0] * 4).cpu(), q),
+                 lambda: hb.hs_rotary(ctx, rope, i32([0] * 4), q, k.cpu()), lambda: hb.hs_rotary_tree(ctx, rope, pr, length.cpu(), q, k, max_nodes=4),
+                 lambda: hb.hs_tree_verify_attention_paged(ctx, pr, cache, q, k.cpu(), k, **tree), lambda: hb.hs_tree_verify_attention_paged(ctx, pr, host, q, k, k, **tree),
+                 lambda: hb.hs_tree_verify_attention_paged(ctx, pr, cache, q, k, k, lse_out=torch.zeros(4, 8), **tree)):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert hb.hs_device_error(ctx) == 0
+    ctx.close()

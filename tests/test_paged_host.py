@@ -250,3 +250,17 @@ def test_lists_of_one_entry_have_no_stride():
     assert one.stride() == (3,)
     assert hb.native().kv_append(0, c, rows(), rows(), off, one, 0) == hb.HS_ERR_INVALID_ARG
     assert hb.native().rotary(0, hb.make_rope(128), one, rows(1), rows(1), None, None, 0) == hb.HS_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("call", [
+    lambda n, x, c, pr, acc, o: n.kv_append(x, c, rows(), rows(), o, None, 0),
+    lambda n, x, c, pr, acc, o: n.kv_append_path(x, c, pr, acc, 0, None, rows(), rows(), None, 0),
+    lambda n, x, c, pr, acc, o: n.kv_read(x, c, o, None, rows(), rows(), 0),
+    lambda n, x, c, pr, acc, o: n.tree_verify_attention_paged(x, pr, c, rows(), rows(), rows(), 4, 9, 0, None, None, rows(), None, 0),
+    lambda n, x, c, pr, acc, o: n.rotary(x, hb.make_rope(128), o, rows(3), rows(3), rows(3), rows(3), 0),
+    lambda n, x, c, pr, acc, o: n.rotary_tree(x, hb.make_rope(128), pr, c.kv_len, 4, 0, None, rows(), rows(), None, None, 0),
+])
+def test_tensors_in_host_memory_are_python_errors(call):
+    context = (ctypes.c_char * 1024)()                                   # of device 0
+    with pytest.raises(ValueError):
+        call(hb.native(), ctypes.addressof(context), cache(), hb.PrunedTree(4, 2, "cpu"), hb.AcceptOut(2, 4, "cpu"), torch.zeros(3, dtype=torch.int32))
