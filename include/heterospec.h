@@ -350,7 +350,7 @@ hs_status hs_cart_fit(hs_ctx* ctx, const float* x, const float* y, int32_t n, in
  * keep the cache).  Every (token, kv head) holds 128 values x as E4M3 bytes and one E8M0 byte s:
  *   e = the least integer with max|x| <= 448 * 2^e, in [-126, 127];  byte_i = E4M3(x_i * 2^-e), ties to even;  s = e + 127
  * and stands for byte_i * 2^(s - 127).  The scale is a power of two, so scaling is exact: writing rounds once, by at
- * most 2^-4 of a value (2^-10 * 2^e for the smallest), reading not at all.  A row with a value that is not finite gets
+ * most 2^-4 of a value (2^-10 * 2^e for the smallest), reading not at all (bf16: from 2^-130 on).  A row with a value that is not finite gets
  * s = 255 and reads as NaN in all of its values.  (The bytes 0x7f and 0xff, E4M3's NaN, are written in such rows only; what a cache filled by
  * other hands means by them in other rows is not defined.)
  *   token t of sequence b = slot t % page_size of page page_table[b * max_pages + t / page_size];
@@ -395,8 +395,8 @@ hs_status hs_kv_append_path(hs_ctx* ctx, const hs_kv_cache* cache, const hs_prun
                             const void* v_tree, int32_t max_rows, int32_t* len_out, hs_stream stream);
 
 /* Reads back: row row_off[b] + i of k_out, v_out (bf16 or f32, strides as for hs_kv_append) = token first[b] + i of sequence b
- * (first NULL: 0).  Rows of tokens outside [0, kv_len[b]) and rows from row_off[batch] on are left as they were.  A value that
- * bf16 holds (every one of 2^-133 and up) is exact. */
+ * (first NULL: 0).  Rows of tokens outside [0, kv_len[b]) and rows from row_off[batch] on are left as they were.  f32 is
+ * exact, bf16 too from 2^-130 on; smaller values are rounded to a multiple of 2^-133. */
 hs_status hs_kv_read(hs_ctx* ctx, const hs_kv_cache* cache, const int32_t* row_off, const int32_t* first, int32_t n_rows,
                      void* k_out, void* v_out, hs_dtype dtype, int64_t token_stride, int64_t head_stride, hs_stream stream);
 

@@ -105,7 +105,7 @@ template <> struct KvBytes<__nv_bfloat16> {
         for (int c = 0; c < 2; ++c) {
             auto pair = [&](unsigned int x) {
                 const float2 v = e4m3_floats(x);
-                __nv_bfloat162 h = __floats2bfloat162_rn(v.x * f, v.y * f);      // exact: four significant bits (below 2^-126 rounded as fp32 would be)
+                __nv_bfloat162 h = __floats2bfloat162_rn(v.x * f, v.y * f);      // exact: four significant bits (below 2^-130 rounded to a multiple of 2^-133)
                 return *reinterpret_cast<unsigned int*>(&h);
             };
             *(reinterpret_cast<uint4*>(row) + c * 8 + sub) = make_uint4(pair(w[c].x), pair(w[c].x >> 16), pair(w[c].y), pair(w[c].y >> 16));

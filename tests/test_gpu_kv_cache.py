@@ -308,3 +308,22 @@ def test_refusals(ctx):
     torch.cuda.synchronize()
     same(cache, before)
     assert hb.hs_device_error(ctx) == 0
+
+
+def test_the_smallest_values_are_read_as_they_are():
+    """All bytes at the smallest scales: fp32 is exact, bf16 from 2^-130 on; below that to a multiple of 2^-133."""
+    ctx, cache = fresh(), hb.KvCache.empty(2, 1, 16, i32([[0, 1]]))
+    cache.k.copy_(torch.arange(256, device="cuda").to(torch.uint8).view(2, 1, 1, 128).expand(2, 1, 16, 128))
+    cache.k_scale.copy_(torch.arange(16, device="cuda").to(torch.uint8).expand(2, 1, 16))
+    cache.k.masked_fill_((cache.k & 127) == 127, 0)
+    cache.kv_len.fill_(32)
+    want = paged.read(cache.k.cpu().numpy(), cache.k_scale.cpu().numpy(), [[0, 1]], 16, 0, range(32))
+    out = [torch.zeros(32, 1, 128, dtype=t, device="cuda") for t in (torch.float32, torch.bfloat16)]
+    for x in out:
+        hb.hs_kv_read(ctx, cache, i32([0, 32]), k_out=x, v_out=torch.zeros_like(x))
+    whole, half = (x.double().cpu().numpy() for x in out)
+    assert np.array_equal(whole, want)
+    large = np.abs(want) >= 2.0 ** -130
+    assert large.any() and (~large).any() and np.array_equal(half[large], want[large])
+    assert np.array_equal(half[~large], np.rint(want[~large] * 2.0 ** 133) * 2.0 ** -133)
+    ctx.close()
