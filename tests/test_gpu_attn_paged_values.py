@@ -195,3 +195,17 @@ def test_huge_values_among_zeros(batch, nodes, hq, hkv, tokens, places, value):
         r = slice(b * nodes, (b + 1) * nodes)
         check(out[r], lse[r], q[r], K, V, k[r], v[r], m)
     ctx.close()
+
+
+def test_more_sequences_than_a_block_has_threads():
+    batch, hkv, lens = 700, 1, [(37 * b) % 90 for b in range(700)]
+    rng = np.random.default_rng(3)
+    cache, K, V = shared_cache(batch, rng.standard_normal((96, hkv, 128)), rng.standard_normal((96, hkv, 128)), page=32)
+    cache.kv_len.copy_(i32(lens))
+    ctx, _, pr = make_trees([1] * batch, 3)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v = (torch.randn(batch, h, 128, device="cuda", generator=g).bfloat16() for h in (4, hkv, hkv))
+    out, lse = run(ctx, pr, cache, q, k, v, [1] * batch)
+    for b in range(batch):
+        check(out[b:b + 1], lse[b:b + 1], q[b:b + 1], K[:lens[b]], V[:lens[b]], k[b:b + 1], v[b:b + 1], np.ones((1, 1), dtype=bool))
+    ctx.close()
