@@ -24,14 +24,15 @@ inline int paged_splits(int blocks, int sm_count, int tiles, const int* cap) {
 }
 
 // pairs: (sequence, kv head); rows: query rows of one pair.
+// (Times back to back, inputs rotating.)
 // Few rows: a block of 32 or 64 holds them four times or twice over, each copy a part of a tile's columns.  Tokens without drafts (four rows), 32 sequences of 1024 to 8192:
-// 78 us in blocks of 32, 88 in blocks of 64, 115 of 128; one token behind 512: 7.7, 8.2, 9.2.  Trees of 16 (64 rows) behind 2048 tokens, 32 sequences: 55 us in blocks of 64, 66 of 128;
-// one: 12.8 and 14.2.
+// 80 us in blocks of 32, 93 in blocks of 64, 106 of 128; one token behind 512: 7.9, 8.1, 9.5.  Trees of 16 (64 rows) behind 2048 tokens, 32 sequences: 58 us in blocks of 64, 65 of 128;
+// one: 12.2 and 13.2.
 // More than 128 rows: a CTA of 256 converts a tile of values once for both halves and takes 1.7 times (short prefixes) to 2 times (long ones) as long as one of 128,
-// so it is taken where blocks of 128 need twice the rounds of the machine.  64 heads over 8, trees of 62, 4096 tokens: 8 sequences 101 us against 109, 4 sequences 98 against 57;
-// 32 heads over 8, trees of 60, 2048 tokens: 16 sequences 60 against 67, 8 sequences 58 against 36.
-// Splits: one token behind 32768 takes 40 us with 8 CTAs a head, 57 with 11 and 48 with 16 (which do not all fit at once); a tree of 60 behind 2048 tokens 17.1 with 6 and 19.3 with 4;
-// 8 sequences of 1000 to 4000 tokens 25 with 2 and 38 with 1.
+// so it is taken where blocks of 128 need twice the rounds of the machine.  64 heads over 8, trees of 62, 4096 tokens: 8 sequences 102 us against 110, 4 sequences 99 against 58;
+// 32 heads over 8, trees of 60, 2048 tokens: 16 sequences 61 against 67, 8 sequences 58 against 36.
+// Splits: one token behind 32768 takes 42 us with 8 CTAs a head, 58 with 11 and 49 with 16 (which do not all fit at once); a tree of 60 behind 2048 tokens 17.0 with 6 and 19.0 with 4;
+// single tokens behind 1000 to 4000, 8 sequences, 26 with 2 and 39 with 1.
 inline PagedChoice paged_choice(int pairs, int rows, int sm_count, int tiles, const int* cap) {
     PagedChoice c;
     auto rounds = [&](int r) { return (pairs * ((rows + r - 1) / r) + sm_count - 1) / sm_count; };

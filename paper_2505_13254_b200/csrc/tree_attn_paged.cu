@@ -26,10 +26,10 @@
 //     quarter of a tile's columns, with a maximum, a sum and an O of its own: a tile's softmax is as many times shorter, and all four schedulers
 //     have a share of it.
 // Registers: 640 threads are launched with 96 each; the softmax warps take 144, what the others give back.
-// What bounds it.  Tokens without drafts: HBM, a tile of keys and values a CTA every 750 clocks of which 665 are the bytes' (32 sequences of 1024 to 8192 tokens, 307 MB: 77 us,
-// 4.0 TB/s with both CTAs' starts and ends; a CTA spends 12000 clocks on those).  Trees behind long prefixes: the softmax warps' instructions (four trees of 62 nodes and 64 heads behind
-// 32768 tokens, 267 GFLOP: 355 us, 0.75 PFLOP/s; an SM issues in 59% of its clocks, the exponential unit is busy in 44%, the products take 512 of a tile's 1300 clocks).  Small calls: the
-// chain from the launch to the merged rows (one token behind 512: 7.7 us; a tree of 60 behind 2048: 16.5 us).
+// What bounds it.  Tokens without drafts: HBM, a tile of keys and values a CTA every 750 clocks of which 665 are the bytes' (32 sequences of 1024 to 8192 tokens, 307 MB: 80 us back to back,
+// 3.8 TB/s with both CTAs' starts and ends; a CTA spends 12000 clocks on those).  Trees behind long prefixes: the softmax warps' instructions (four trees of 62 nodes and 64 heads behind
+// 32768 tokens, 267 GFLOP: 361 us back to back, 0.74 PFLOP/s; an SM issues in 60% of its clocks, the exponential unit is busy in 42%, the products take 512 of a tile's 1300 clocks).  Small calls: the
+// chain from the launch to the merged rows (one token behind 512: 7.8 us; a tree of 60 behind 2048: 16.4 us).
 // Behind the last token and in the last page a tile is zero, whatever the memory holds, and masked.  A tree value that is not finite, or of 2^10 and more, is
 // zero in the product (0 * inf would reach the rows that mask it, and a large one would cost the other columns of the rows that see it their bits) and added to the rows that see it at the end.
 #include <cuda_fp16.h>
@@ -70,7 +70,7 @@ template <int ROWS>
 struct Layout {
     static constexpr bool WIDE = ROWS == 256;
     static constexpr int rows = WIDE ? 256 : 128;
-    // units of V in flight (with four, 32 ragged sequences without drafts take 82 us instead of 77: their bytes take 2300 clocks to come)
+    // units of V in flight (with four, 32 ragged sequences without drafts take 83 us instead of 80: their bytes take 2300 clocks to come)
     static constexpr int units = WIDE ? 4 : 8;
     static_assert(units % PG_GROUPS == 0 && PG_KEYS % 2 == 0, "a unit serves one group: two could not tell its barriers' rounds apart by their parity");
     static constexpr int recv_bytes = PG_ROW_STRIDE * (rows + 2 * PG_MAX_SPLIT);
@@ -280,7 +280,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
     }
     pdl_launch_dependents();
     pdl_wait();
-    // Sequences longest first, so that a ragged batch ends on short ones: slot z / hkv is the sequence of that rank by (length descending, index ascending).
+    // Sequences longest first, so that a ragged batch ends on short ones (more than the block has threads go in their own order): slot z / hkv is the sequence of that rank by (length descending, index ascending).
     int b = blockIdx.z / p.c.hkv;
     const int h = blockIdx.z % p.c.hkv;
     if (p.c.batch > 1 && p.c.batch <= PG_THREADS) {
@@ -339,7 +339,7 @@ tree_attn_paged_kernel(const __grid_constant__ PagedParams p, const __grid_const
 
     // A row of 128 bf16 in two halves of a tile becomes its two terms, 128 bytes each, in their place, by the sixteen lanes that brought it, and 2^e in out[]: NaN where
     // something is not finite, which makes NaN of every score it touches.  Rows first, first + 16, ... (four at most) of those below `rows`: their loads and sums go side by side.
-    // One row at a time in blocks of few rows, where what counts is how little code is fetched (a token behind 512 7.7 us, with four rows side by side, here and below, 8.8); four above
+    // One row at a time in blocks of few rows, where what counts is how little code is fetched (a token behind 512 7.7 us when this was chosen, with four rows side by side, here and below, 8.8); four above
     // (a tree of 60 behind 100 tokens 11.5, with one 12.0).
     constexpr int TERM_ROWS = REP > 1 ? 1 : 4;
     const int sub = tid & 15;
