@@ -29,8 +29,8 @@
 // Registers: 640 threads are launched with 96 each; the softmax warps take 144, what the others give back.
 // What bounds it.  Tokens without drafts: HBM, a tile of keys and values a CTA every 750 clocks of which 665 are the bytes' (32 sequences of 1024 to 8192 tokens, 307 MB: 80 us back to back,
 // 3.8 TB/s with both CTAs' starts and ends; a CTA spends 12000 clocks on those).  Trees behind long prefixes: the softmax warps' instructions (four trees of 62 nodes and 64 heads behind
-// 32768 tokens, 267 GFLOP: 361 us back to back, 0.74 PFLOP/s; an SM issues in 60% of its clocks, the exponential unit is busy in 42%, the products take 512 of a tile's 1300 clocks).  Small calls: the
-// chain from the launch to the merged rows (one token behind 512: 7.8 us; a tree of 60 behind 2048: 16.4 us).
+// 32768 tokens, 267 GFLOP: 362 us back to back, 0.74 PFLOP/s; an SM issues in 60% of its clocks, the exponential unit is busy in 42%, the products take 512 of a tile's 1300 clocks).  Small calls: the
+// chain from the launch to the merged rows (one token behind 512: 7.7 us; a tree of 60 behind 2048: 16.5 us).
 // Behind the last token and in the last page a tile is zero, whatever the memory holds, and masked.  A tree value that is not finite, or of 2^10 and more, is
 // zero in the product (0 * inf would reach the rows that mask it, and a large one would cost the other columns of the rows that see it their bits) and added to the rows that see it at the end.
 #include <cuda_fp16.h>
